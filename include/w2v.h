@@ -468,6 +468,72 @@ int w2v_step_batch_sorted(int32_t B, int32_t N, int32_t K, const int32_t* target
                           void* workspace, size_t workspace_bytes, int64_t* stats,
                           void* stream);
 
+/*
+ * The vocabulary head: what a trained model answers with. Scores of contexts
+ * against the rows of M_out are a matrix product; a smaller model learns
+ * another one's distribution from its top scores; words are drawn from
+ * scores. (Not in the paper, which ends with the trained vectors.)
+ *
+ * Matrices are row-major with unit column stride and a row stride in
+ * elements, at least the number of columns, of any alignment that one element
+ * has; row offsets are 64-bit. Element types:
+ */
+#define W2V_DTYPE_F32 0
+#define W2V_DTYPE_BF16 1
+#define W2V_DTYPE_F16 2
+
+/* The `activation` argument of w2v_linear. */
+#define W2V_ACTIVATION_NONE 0
+#define W2V_ACTIVATION_RELU 1
+#define W2V_ACTIVATION_GELU 2 /* z Phi(z), with the error function */
+#define W2V_ACTIVATION_SILU 3 /* z sigma(z) */
+#define W2V_ACTIVATION_TANH 4
+#define W2V_ACTIVATION_SIGMOID 5
+
+/*
+ * y = act(x W^T + b) + residual, for x M x K, W N x K (a row per output, as
+ * M_out holds a row per word) and y M x N.
+ *   dtype         type of x, W and pre (W2V_DTYPE_*);
+ *   out_dtype     type of y and residual: dtype or W2V_DTYPE_F32;
+ *   bias          device float[N] or NULL;
+ *   residual      device M x N or NULL; may be y itself;
+ *   pre           device M x N or NULL: receives z = x W^T + b, which
+ *                 w2v_linear_backward needs where there is an activation.
+ * Sums and the epilogue are held in fp32 and each output is rounded once. The
+ * order of a sum depends on the sizes alone: the same call gives the same
+ * bits. workspace: device, 256-byte aligned, at least
+ * w2v_linear_workspace_bytes(M, N, K, dtype) bytes (0 unless a long k is
+ * split), contents need not be initialised; calls that overlap in time must
+ * not share it. M = 0 is allowed and does nothing; N, K >= 1. y and pre must
+ * not overlap any other argument (residual = y excepted).
+ */
+size_t w2v_linear_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t dtype);
+int w2v_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, const float* bias,
+               const void* residual, int64_t ldr, void* y, int64_t ldy, void* pre,
+               int64_t ldp, int32_t M, int32_t N, int32_t K, int32_t dtype,
+               int32_t out_dtype, int32_t activation, void* workspace,
+               size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of w2v_linear from dy (M x N):
+ *   dz = dy * act'(pre), dx = dz W (M x K), dW = dz^T x (N x K),
+ *   db = sum over the rows of dz (device float[N]);
+ * the residual's gradient is dy itself. dx, dw and db may each be NULL (not
+ * wanted). pre: z as w2v_linear wrote it, needed unless the activation is
+ * W2V_ACTIVATION_NONE; relu's derivative at 0 is 0. All matrices are of
+ * `dtype`. With an activation, dz is rounded once to `dtype`; sums are held in
+ * fp32, in an order that depends on the sizes alone. M = 0 gives dW = 0 and
+ * db = 0. workspace: as above, w2v_linear_backward_workspace_bytes bytes.
+ * Outputs must not overlap any other argument.
+ */
+size_t w2v_linear_backward_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t dtype,
+                                           int32_t activation);
+int w2v_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                        const void* w, int64_t ldw, const void* pre, int64_t ldp, void* dx,
+                        int64_t lddx, void* dw, int64_t lddw, float* db, int32_t M, int32_t N,
+                        int32_t K, int32_t dtype, int32_t activation, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

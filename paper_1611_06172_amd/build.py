@@ -18,7 +18,8 @@ MEASURE_LIB = os.path.join(HERE, "libw2v_measure.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 HIP_SOURCES = ["api.hip", "epoch_kernels.hip", "pairwise_kernels.hip",
-               "step_kernels.hip", "step_sorted.hip", "vocab.hip", "radix_sort.hip"]
+               "step_kernels.hip", "step_sorted.hip", "vocab.hip", "radix_sort.hip",
+               "head_api.hip", "linear.hip"]
 CXX_SOURCES = ["tables.cpp"]
 
 HIP_FLAGS = [

@@ -130,6 +130,12 @@ static int enter_device(int32_t** status_dev, void** scratch_dev = nullptr,
   return W2V_OK;
 }
 
+int enter_call(int32_t** status_dev) { return enter_device(status_dev); }
+
+int launch_failed(int hip_error, const char* what) {
+  return hip_fail((hipError_t)hip_error, what);
+}
+
 // Compute units of the current device (queried once per device).
 static int cu_count() {
   static std::mutex mu;

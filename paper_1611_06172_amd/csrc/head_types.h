@@ -1,0 +1,114 @@
+// Element types, wide loads and stores, activations and launch helpers shared
+// by the kernels of the vocabulary head (linear.hip, distill.hip,
+// sample.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "w2v.h"
+
+namespace w2v {
+
+typedef __bf16 bf16_t;
+typedef _Float16 f16_t;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(bf16_t v) {
+  return __builtin_bit_cast(float, (uint32_t)__builtin_bit_cast(uint16_t, v) << 16);
+}
+__device__ __forceinline__ float to_f32(f16_t v) { return (float)v; }
+
+// One rounding to nearest even from 32 bits.
+template <typename T>
+__device__ __forceinline__ T from_f32(float v) {
+  return (T)v;
+}
+
+// N consecutive elements at an address aligned to one element. gfx950 loads
+// and stores up to 16 bytes at any alignment in one instruction, so rows of
+// odd strides take the same path as aligned ones.
+template <typename T, int N>
+struct Pack {
+  T v[N];
+};
+
+template <typename T, int N>
+__device__ __forceinline__ Pack<T, N> load_pack(const T* p) {
+  Pack<T, N> out;
+  __builtin_memcpy(&out, p, sizeof(out));
+  return out;
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& v) {
+  __builtin_memcpy(p, &v, sizeof(v));
+}
+
+// The first n (0..N) elements at p, the others 0.
+template <typename T, int N>
+__device__ __forceinline__ Pack<T, N> load_some(const T* p, int64_t n) {
+  if (n >= N) return load_pack<T, N>(p);
+  Pack<T, N> out;
+#pragma unroll
+  for (int i = 0; i < N; i++) out.v[i] = i < n ? p[i] : T(0.0f);
+  return out;
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_some(T* p, int64_t n, const Pack<T, N>& v) {
+  if (n >= N) {
+    store_pack<T, N>(p, v);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < N; i++)
+    if (i < n) p[i] = v.v[i];
+}
+
+__device__ __forceinline__ float activate(float z, int activation) {
+  switch (activation) {
+    case W2V_ACTIVATION_RELU:
+      return z < 0.0f ? 0.0f : z;  // NaN stays NaN
+    case W2V_ACTIVATION_GELU:
+      return 0.5f * z * erfcf(z * -0.70710678118654752f);
+    case W2V_ACTIVATION_SILU:
+      return z / (1.0f + expf(-z));
+    case W2V_ACTIVATION_TANH:
+      return tanhf(z);
+    case W2V_ACTIVATION_SIGMOID:
+      return 1.0f / (1.0f + expf(-z));
+    default:
+      return z;
+  }
+}
+
+// Derivative of `activate` at z. relu's at 0 is 0.
+__device__ __forceinline__ float activation_slope(float z, int activation) {
+  switch (activation) {
+    case W2V_ACTIVATION_RELU:
+      return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
+    case W2V_ACTIVATION_GELU:
+      return 0.5f * erfcf(z * -0.70710678118654752f) +
+             z * expf(-0.5f * z * z) * 0.39894228040143268f;
+    case W2V_ACTIVATION_SILU: {
+      const float p = 1.0f / (1.0f + expf(-z));
+      const float q = 1.0f / (1.0f + expf(z));  // 1 - p without cancellation
+      return p + z * p * q;
+    }
+    case W2V_ACTIVATION_TANH: {
+      const float t = tanhf(z);
+      return (1.0f - t) * (1.0f + t);
+    }
+    case W2V_ACTIVATION_SIGMOID:
+      return (1.0f / (1.0f + expf(-z))) * (1.0f / (1.0f + expf(z)));
+    default:
+      return 1.0f;
+  }
+}
+
+}  // namespace w2v

@@ -14,6 +14,12 @@ int fail(int code, const char* msg);
 int failf(int code, const char* fmt, ...);
 // Clears this thread's last error and returns W2V_OK.
 int ok();
+// Entry check of a GPU call from another source file: sets up the current
+// device if needed, reports an earlier call's skipped work, and gives the
+// device address of the error word.
+int enter_call(int32_t** status_dev);
+// Records a HIP error (a hipError_t) and returns W2V_EHIP.
+int launch_failed(int hip_error, const char* what);
 
 int hot_rows(const int64_t* counts, int32_t V, double power, double sample_t,
              int32_t window, int32_t K, int64_t inflight, double tol);

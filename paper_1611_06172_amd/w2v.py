@@ -98,6 +98,18 @@ def lib():
     L.w2v_step_batch_sorted_workspace_bytes.restype = ctypes.c_size_t
     L.w2v_step_batch_sorted.argtypes = L.w2v_step_batch.argtypes
     L.w2v_step_batch_sorted.restype = ctypes.c_int
+    L.w2v_linear_workspace_bytes.argtypes = [_i32, _i32, _i32, _i32]
+    L.w2v_linear_workspace_bytes.restype = ctypes.c_size_t
+    L.w2v_linear.argtypes = [
+        _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _i32,
+        _i32, _i32, _i32, _vp, ctypes.c_size_t, _vp]
+    L.w2v_linear.restype = ctypes.c_int
+    L.w2v_linear_backward_workspace_bytes.argtypes = [_i32, _i32, _i32, _i32, _i32]
+    L.w2v_linear_backward_workspace_bytes.restype = ctypes.c_size_t
+    L.w2v_linear_backward.argtypes = [
+        _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _i32,
+        _i32, _i32, _i32, _vp, ctypes.c_size_t, _vp]
+    L.w2v_linear_backward.restype = ctypes.c_int
     _lib = L
     return L
 
@@ -490,3 +502,170 @@ def build_vocab(raw, V_raw: int, min_count: int = 0, remap: bool = True,
                                  ws.numel(), _stream(stream)))
     return dict(ranked_counts=ranked, rank_of=rank_of, corpus=corpus,
                 V=int(v_kept.item()))
+
+
+# ------------------------------------------------------ the vocabulary head --
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "tanh": 4, "sigmoid": 5}
+
+
+def _dtypes():
+    import torch
+    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _head_dtype(t, name):
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.dtype not in _dtypes():
+        raise TypeError(f"{name} must have dtype float32, bfloat16 or float16, got {t.dtype}")
+    return _dtypes()[t.dtype]
+
+
+def _operand(t, name, shape=None, dtype=None):
+    """Row stride of a 2-D GPU matrix whose columns are adjacent."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be 2-D")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    _here(t, name)
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit column stride")
+    if rows <= 1:
+        return max(cols, 1)
+    if t.stride(0) < cols:
+        raise ValueError(f"{name} must have a row stride >= its columns")
+    return t.stride(0)
+
+
+def _here(t, name):
+    import torch
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current device")
+
+
+def _vector(t, dtype, name, n):
+    _dev(t, dtype, name, 1)
+    _here(t, name)
+    if t.numel() != n:
+        raise ValueError(f"{name} must have {n} entries")
+    return t
+
+
+def _allocations(stream):
+    """Makes the call's stream current, so that what the binding allocates
+    belongs to it and is not handed out again before its work is done."""
+    import contextlib
+
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _head_workspace(need, workspace, device):
+    """The caller's workspace (the library checks its size), or one of `need`
+    bytes."""
+    import torch
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _dev(workspace, torch.uint8, "workspace", 1)
+    _here(workspace, "workspace")
+    return workspace
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {name!r}")
+    return ACTIVATIONS[name]
+
+
+def linear_workspace_bytes(M: int, N: int, K: int, dtype) -> int:
+    return int(lib().w2v_linear_workspace_bytes(M, N, K, _dtypes()[dtype]))
+
+
+def linear_backward_workspace_bytes(M: int, N: int, K: int, dtype,
+                                    activation: str = "none") -> int:
+    return int(lib().w2v_linear_backward_workspace_bytes(M, N, K, _dtypes()[dtype],
+                                                         _activation(activation)))
+
+
+def linear(x, weight, bias=None, *, activation: str = "none", residual=None,
+           out_dtype=None, out=None, pre=None, workspace=None, stream=None):
+    """act(x weight^T + bias) + residual (w2v_linear).
+
+    x (M, K) and weight (N, K) are float32, bfloat16 or float16, rows may be
+    padded (a trained M_out of alloc_matrix is a weight); bias float32 (N,);
+    residual (M, N) in the output's type. out_dtype: x's type (the default)
+    or float32. out: receives the result (may be the residual itself). pre:
+    an (M, N) tensor of x's type that receives the sum before the
+    activation, for linear_backward."""
+    import torch
+    code = _head_dtype(x, "x")
+    ldx = _operand(x, "x")
+    M, K = x.shape
+    ldw = _operand(weight, "weight", dtype=x.dtype)
+    N = weight.shape[0]
+    if weight.shape[1] != K:
+        raise ValueError("x and weight must have the same number of columns")
+    if bias is not None:
+        _vector(bias, torch.float32, "bias", N)
+    if out is not None:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError("out and out_dtype disagree")
+        out_dtype = out.dtype
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    if out_dtype not in (x.dtype, torch.float32):
+        raise TypeError("out_dtype must be x's dtype or float32")
+    act = _activation(activation)
+    ldr = N if residual is None else _operand(residual, "residual", (M, N), out_dtype)
+    ldp = N if pre is None else _operand(pre, "pre", (M, N), x.dtype)
+    with _allocations(stream):
+        if out is None:
+            out = torch.empty((M, N), dtype=out_dtype, device=x.device)
+        ldy = _operand(out, "out", (M, N), out_dtype)
+        ws = _head_workspace(linear_workspace_bytes(M, N, K, x.dtype), workspace, x.device)
+        _check(lib().w2v_linear(
+            _ptr(x), ldx, _ptr(weight), ldw, _ptr(bias), _ptr(residual), ldr, _ptr(out), ldy,
+            _ptr(pre), ldp, M, N, K, code, _dtypes()[out_dtype], act, _ptr(ws),
+            0 if ws is None else ws.numel(), _stream(stream)))
+    return out
+
+
+def linear_backward(dy, x, weight, *, activation: str = "none", pre=None,
+                    want_dx: bool = True, want_dw: bool = True, want_db: bool = True,
+                    workspace=None, stream=None):
+    """Gradients of linear() from dy (M, N): a dict of dx (M, K) and dw (N, K)
+    in x's type and db float32 (N,), None where not wanted
+    (w2v_linear_backward). pre: what linear() wrote, needed with an
+    activation. The residual's gradient is dy."""
+    import torch
+    code = _head_dtype(x, "x")
+    ldx = _operand(x, "x")
+    M, K = x.shape
+    ldw = _operand(weight, "weight", dtype=x.dtype)
+    N = weight.shape[0]
+    if weight.shape[1] != K:
+        raise ValueError("x and weight must have the same number of columns")
+    lddy = _operand(dy, "dy", (M, N), x.dtype)
+    act = _activation(activation)
+    if act != 0 and pre is None:
+        raise ValueError("pre is needed with an activation")
+    ldp = N if pre is None else _operand(pre, "pre", (M, N), x.dtype)
+    with _allocations(stream):
+        out = dict(
+            dx=torch.empty((M, K), dtype=x.dtype, device=x.device) if want_dx else None,
+            dw=torch.empty((N, K), dtype=x.dtype, device=x.device) if want_dw else None,
+            db=torch.empty(N, dtype=torch.float32, device=x.device) if want_db else None)
+        ws = _head_workspace(linear_backward_workspace_bytes(M, N, K, x.dtype, activation),
+                             workspace, x.device)
+        _check(lib().w2v_linear_backward(
+            _ptr(dy), lddy, _ptr(x), ldx, _ptr(weight), ldw, _ptr(pre), ldp, _ptr(out["dx"]),
+            K, _ptr(out["dw"]), K, _ptr(out["db"]), M, N, K, code, act, _ptr(ws),
+            0 if ws is None else ws.numel(), _stream(stream)))
+    return out
