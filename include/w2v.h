@@ -534,6 +534,100 @@ int w2v_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx
                         int32_t K, int32_t dtype, int32_t activation, void* workspace,
                         size_t workspace_bytes, void* stream);
 
+/*
+ * Distillation from a teacher's top logits. Per row, with s the student's V
+ * scores, (id_k, t_k) the teacher's K entries and T the temperature:
+ *   q   = softmax of t / T over the entries that are present,
+ *   p_T = softmax(s / T), p_1 = softmax(s), both over all V words,
+ *   loss = soft T^2 sum_k q_k (log q_k - log p_T(id_k)) - hard log p_1(label).
+ *   logits     device rows x V of `dtype`, stride ld; -inf masks a word;
+ *   ids        device int32[rows][K]: words, -1 = absent entry (its logit is
+ *              not looked at); a row may have none (no soft term). Entries of
+ *              one word add up;
+ *   teacher    device [rows][K] of teacher_dtype: the teacher's logits; -inf
+ *              gives q = 0;
+ *   labels     device int32[rows] or NULL (no hard term); -1 = none;
+ *   row_weight device float[rows] or NULL (1): scales the row's gradient, not
+ *              its loss;
+ *   loss       device float[rows];
+ *   stats      device float[rows][3]: the maximum m of s, log sum
+ *              exp((s - m) / T), and log sum exp(s - m) (with labels, else 0):
+ *              what w2v_distill_backward needs;
+ *   grad       device rows x V of `dtype`, stride ldg, or NULL (not wanted):
+ *              row_weight (soft T (Q p_T - q) + hard (p_1 - [label])), Q = 1 if
+ *              the row has an entry, else 0. May be the logits' own memory
+ *              (same stride), not overlap them otherwise.
+ * A row whose scores are all -inf has loss 0 and gradient 0. NaN or +inf
+ * among a row's scores or present teacher logits makes its loss NaN. A row
+ * with an id or a label outside [-1, V) has loss 0 and gradient 0 and is
+ * recorded in the device's error word. Sums, statistics and loss are held in
+ * fp32; the gradient is rounded once. The same call gives the same bits.
+ * Limits: 0 <= K <= W2V_MAX_TEACHER, temperature in [2^-20, 2^20], rows >= 0,
+ * V >= 1. workspace: device, 256-byte aligned, at least
+ * w2v_distill_workspace_bytes(rows, V, dtype) bytes, contents need not be
+ * initialised; calls that overlap in time must not share it.
+ */
+#define W2V_MAX_TEACHER 1024
+
+size_t w2v_distill_workspace_bytes(int32_t rows, int32_t V, int32_t dtype);
+int w2v_distill_loss(const void* logits, int64_t ld, int32_t rows, int32_t V, int32_t dtype,
+                     const int32_t* ids, const void* teacher, int32_t K,
+                     int32_t teacher_dtype, const int32_t* labels, float temperature,
+                     float soft, float hard, const float* row_weight, float* loss,
+                     float* stats, void* grad, int64_t ldg, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/* The gradient of w2v_distill_loss alone, from the stats that it wrote for
+ * the same logits, temperature and labels: grad = dloss_n d loss_n / d s, with
+ * dloss device float[rows]. */
+int w2v_distill_backward(const float* dloss, const void* logits, int64_t ld, int32_t rows,
+                         int32_t V, int32_t dtype, const int32_t* ids, const void* teacher,
+                         int32_t K, int32_t teacher_dtype, const int32_t* labels,
+                         float temperature, float soft, float hard, const float* stats,
+                         void* grad, int64_t ldg, void* stream);
+
+/*
+ * Words drawn from scores by given random numbers. Per row, with z the V
+ * scores and m their maximum: x_j = (z_j - m) / T, w_j = exp(x_j). Words are
+ * ranked by score, equal ones by index. Kept are the words whose rank is
+ * below top_k, for which the weight of the words ranked before them is below
+ * top_p times the weight of the top_k words, and whose w_j >= min_p; the first
+ * is always kept. Of these the word with the largest x_j - log(-log u_j) is
+ * drawn (the lowest index of equal ones): word j with probability w_j over
+ * the kept words' weight, if the u_j are independent and uniform in (0, 1).
+ *   logits    device rows x V of `dtype`, stride ld; -inf masks a word;
+ *   uniforms  device float rows x V, stride ldu; may be NULL if temperature
+ *             is the scalar 0. Of a row with filters only the kept words'
+ *             numbers are read;
+ *   temperatures, top_ks, top_ps, min_ps  device arrays of `rows` settings,
+ *             each NULL to use the scalar after it for every row.
+ *             Temperature 0 takes the best-ranked word; top_k 0, top_p >= 1
+ *             and min_p 0 are off; top_k is at most W2V_MAX_TOP_K, or >= V,
+ *             which is off;
+ *   ids       device int32[rows]; logprob device float[rows] or NULL: x - log
+ *             sum of all w, the word's log-probability at T before the filters
+ *             (0 at temperature 0).
+ * A row without a word above -inf, or with NaN among its scores, gets id -1
+ * and logprob NaN. Words at +inf weigh 1 each and all others 0. A row whose
+ * setting in an array is invalid (temperature not finite or < 0, top_k < 0 or
+ * between W2V_MAX_TOP_K and V, top_p <= 0 or NaN, min_p outside [0, 1]) gets
+ * the same and is recorded in the device's error word; invalid scalars are
+ * W2V_EINVAL. A u_j of 0 or NaN loses against every other word. Weights are
+ * summed in 64-bit fixed point of at least 2^-31 of the first word's weight,
+ * so nothing depends on an order. workspace: device, 256-byte aligned, at
+ * least w2v_sample_workspace_bytes(rows, V) bytes, contents need not be
+ * initialised; calls that overlap in time must not share it.
+ */
+#define W2V_MAX_TOP_K 1024
+
+size_t w2v_sample_workspace_bytes(int32_t rows, int32_t V);
+int w2v_sample_words(const void* logits, int64_t ld, const float* uniforms, int64_t ldu,
+                     int32_t rows, int32_t V, int32_t dtype, const float* temperatures,
+                     float temperature, const int32_t* top_ks, int32_t top_k,
+                     const float* top_ps, float top_p, const float* min_ps, float min_p,
+                     int32_t* ids, float* logprob, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,7 +19,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 HIP_SOURCES = ["api.hip", "epoch_kernels.hip", "pairwise_kernels.hip",
                "step_kernels.hip", "step_sorted.hip", "vocab.hip", "radix_sort.hip",
-               "head_api.hip", "linear.hip"]
+               "head_api.hip", "linear.hip", "distill.hip", "sample.hip"]
 CXX_SOURCES = ["tables.cpp"]
 
 HIP_FLAGS = [

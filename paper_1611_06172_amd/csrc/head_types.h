@@ -111,4 +111,39 @@ __device__ __forceinline__ float activation_slope(float z, int activation) {
   }
 }
 
+// Reductions over a wavefront and over a block of up to 16 of them; every
+// thread gets the result. `scratch`: 16 floats of LDS, free again on return.
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+__device__ __forceinline__ float block_sum(float v, float* scratch) {
+  v = wave_sum(v);
+  if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = scratch[0];
+  for (int w = 1; w < (int)(blockDim.x >> 6); w++) v += scratch[w];
+  __syncthreads();
+  return v;
+}
+__device__ __forceinline__ float block_max(float v, float* scratch) {
+  v = wave_max(v);
+  if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = scratch[0];
+  for (int w = 1; w < (int)(blockDim.x >> 6); w++) v = fmaxf(v, scratch[w]);
+  __syncthreads();
+  return v;
+}
+
+constexpr float kLog2e = 1.44269504088896341f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
 }  // namespace w2v

@@ -110,6 +110,22 @@ def lib():
         _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _i32,
         _i32, _i32, _i32, _vp, ctypes.c_size_t, _vp]
     L.w2v_linear_backward.restype = ctypes.c_int
+    L.w2v_distill_workspace_bytes.argtypes = [_i32, _i32, _i32]
+    L.w2v_distill_workspace_bytes.restype = ctypes.c_size_t
+    L.w2v_distill_loss.argtypes = [
+        _vp, _i64, _i32, _i32, _i32, _vp, _vp, _i32, _i32, _vp, _f32, _f32, _f32, _vp, _vp,
+        _vp, _vp, _i64, _vp, ctypes.c_size_t, _vp]
+    L.w2v_distill_loss.restype = ctypes.c_int
+    L.w2v_distill_backward.argtypes = [
+        _vp, _vp, _i64, _i32, _i32, _i32, _vp, _vp, _i32, _i32, _vp, _f32, _f32, _f32, _vp,
+        _vp, _i64, _vp]
+    L.w2v_distill_backward.restype = ctypes.c_int
+    L.w2v_sample_workspace_bytes.argtypes = [_i32, _i32]
+    L.w2v_sample_workspace_bytes.restype = ctypes.c_size_t
+    L.w2v_sample_words.argtypes = [
+        _vp, _i64, _vp, _i64, _i32, _i32, _i32, _vp, _f32, _vp, _i32, _vp, _f32, _vp, _f32,
+        _vp, _vp, _vp, ctypes.c_size_t, _vp]
+    L.w2v_sample_words.restype = ctypes.c_int
     _lib = L
     return L
 
@@ -669,3 +685,129 @@ def linear_backward(dy, x, weight, *, activation: str = "none", pre=None,
             K, _ptr(out["dw"]), K, _ptr(out["db"]), M, N, K, code, act, _ptr(ws),
             0 if ws is None else ws.numel(), _stream(stream)))
     return out
+
+
+def _teacher_list(logits, teacher_ids, teacher_logits, labels):
+    """Checked arguments that both distillation calls share, in the library's
+    order."""
+    import torch
+    code = _head_dtype(logits, "logits")
+    ld = _operand(logits, "logits")
+    rows, V = logits.shape
+    _dev(teacher_ids, torch.int32, "teacher_ids", 2)
+    _here(teacher_ids, "teacher_ids")
+    _head_dtype(teacher_logits, "teacher_logits")
+    _dev(teacher_logits, teacher_logits.dtype, "teacher_logits", 2)
+    _here(teacher_logits, "teacher_logits")
+    if teacher_ids.shape[0] != rows or teacher_logits.shape != teacher_ids.shape:
+        raise ValueError("teacher_ids and teacher_logits must have a row per row of logits")
+    if labels is not None:
+        _vector(labels, torch.int32, "labels", rows)
+    return (_ptr(logits), ld, rows, V, code, _ptr(teacher_ids), _ptr(teacher_logits),
+            teacher_ids.shape[1], _dtypes()[teacher_logits.dtype], _ptr(labels))
+
+
+def distill_workspace_bytes(rows: int, V: int, dtype) -> int:
+    return int(lib().w2v_distill_workspace_bytes(rows, V, _dtypes()[dtype]))
+
+
+def distill_loss(logits, teacher_ids, teacher_logits, *, temperature: float = 1.0,
+                 labels=None, soft: float = 1.0, hard: float = 0.0, row_weight=None,
+                 want_grad: bool = False, grad=None, workspace=None, stream=None):
+    """Distillation from a teacher's top logits (w2v_distill_loss): a dict of
+    loss float32 (rows,), stats float32 (rows, 3) for distill_backward, and
+    grad (logits' shape and type) or None.
+
+    logits (rows, V) float32, bfloat16 or float16, rows may be padded;
+    teacher_ids int32 (rows, K), -1 absent; teacher_logits (rows, K) of any of
+    the three types; labels int32 (rows,), -1 none. The loss of a row is soft
+    T^2 KL(teacher || student at T) + hard (-log p(label)). want_grad: the
+    gradient of the losses' sum, each row's scaled by row_weight (float32
+    (rows,), 1 if None). grad: receives it (logits itself: in place)."""
+    import torch
+    head = _teacher_list(logits, teacher_ids, teacher_logits, labels)
+    rows = logits.shape[0]
+    if row_weight is not None:
+        _vector(row_weight, torch.float32, "row_weight", rows)
+    with _allocations(stream):
+        if want_grad and grad is None:
+            grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        ldg = 0 if grad is None else _operand(grad, "grad", logits.shape, logits.dtype)
+        loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
+        stats = torch.empty((rows, 3), dtype=torch.float32, device=logits.device)
+        ws = _head_workspace(distill_workspace_bytes(rows, logits.shape[1], logits.dtype),
+                             workspace, logits.device)
+        _check(lib().w2v_distill_loss(
+            *head, float(temperature), float(soft), float(hard), _ptr(row_weight), _ptr(loss),
+            _ptr(stats), _ptr(grad), ldg, _ptr(ws), 0 if ws is None else ws.numel(),
+            _stream(stream)))
+    return dict(loss=loss, stats=stats, grad=grad)
+
+
+def distill_backward(dloss, logits, teacher_ids, teacher_logits, stats, *,
+                     temperature: float = 1.0, labels=None, soft: float = 1.0,
+                     hard: float = 0.0, grad=None, stream=None):
+    """Gradient of distill_loss() for the losses' gradients dloss float32
+    (rows,), from its stats (w2v_distill_backward); the other arguments as
+    they were there. grad: receives it (logits itself: in place)."""
+    import torch
+    head = _teacher_list(logits, teacher_ids, teacher_logits, labels)
+    rows = logits.shape[0]
+    _vector(dloss, torch.float32, "dloss", rows)
+    _dev(stats, torch.float32, "stats", 2)
+    _here(stats, "stats")
+    if tuple(stats.shape) != (rows, 3):
+        raise ValueError("stats must have shape (rows, 3)")
+    with _allocations(stream):
+        if grad is None:
+            grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        ldg = _operand(grad, "grad", logits.shape, logits.dtype)
+        _check(lib().w2v_distill_backward(
+            _ptr(dloss), *head, float(temperature), float(soft), float(hard), _ptr(stats),
+            _ptr(grad), ldg, _stream(stream)))
+    return grad
+
+
+MAX_TOP_K = 1024
+
+
+def sample_workspace_bytes(rows: int, V: int) -> int:
+    return int(lib().w2v_sample_workspace_bytes(rows, V))
+
+
+def sample_words(logits, uniforms=None, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                 want_logprob: bool = True, workspace=None, stream=None):
+    """Draws a word from each row of scores (w2v_sample_words): a dict of ids
+    int32 (rows,) and logprob float32 (rows,) or None.
+
+    logits (rows, V) float32, bfloat16 or float16, -inf masks a word; uniforms
+    float32 (rows, V), independent random numbers in (0, 1) (not needed at
+    temperature 0). temperature, top_k, top_p and min_p are numbers, or
+    tensors of one setting per row (float32; top_k int32). 0 for the
+    temperature takes the best word; top_k 0, top_p 1 and min_p 0 are off. A
+    row without a word gets id -1."""
+    import torch
+    code = _head_dtype(logits, "logits")
+    ld = _operand(logits, "logits")
+    rows, V = logits.shape
+    ldu = V if uniforms is None else _operand(uniforms, "uniforms", (rows, V), torch.float32)
+
+    def setting(v, name, dtype, kind):
+        if isinstance(v, torch.Tensor):
+            return _ptr(_vector(v, dtype, name, rows)), kind(0)
+        return None, kind(v)
+
+    t = setting(temperature, "temperature", torch.float32, float)
+    k = setting(top_k, "top_k", torch.int32, int)
+    p = setting(top_p, "top_p", torch.float32, float)
+    least = setting(min_p, "min_p", torch.float32, float)
+    with _allocations(stream):
+        ids = torch.empty(rows, dtype=torch.int32, device=logits.device)
+        logprob = torch.empty(rows, dtype=torch.float32, device=logits.device) \
+            if want_logprob else None
+        ws = _head_workspace(sample_workspace_bytes(rows, V), workspace, logits.device)
+        _check(lib().w2v_sample_words(
+            _ptr(logits), ld, _ptr(uniforms), ldu, rows, V, code, *t, *k, *p, *least,
+            _ptr(ids), _ptr(logprob), _ptr(ws), 0 if ws is None else ws.numel(),
+            _stream(stream)))
+    return dict(ids=ids, logprob=logprob)

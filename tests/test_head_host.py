@@ -73,3 +73,60 @@ def test_linear_workspaces():
         64, 71_290, 300, torch.bfloat16, "silu") >= n + 64 * 71_290 * 2
     assert w2v.lib().w2v_linear_workspace_bytes(-1, 5, 5, 0) == 0
     assert w2v.lib().w2v_linear_workspace_bytes(1, 5, 5, 7) == 0
+
+
+def distill_args(**over):
+    args = dict(logits=FAKE, ld=100, rows=4, V=100, dtype=0, ids=FAKE, teacher=FAKE, K=8,
+                tdtype=0, labels=None, T=2.0, soft=1.0, hard=0.0, weight=None, loss=FAKE,
+                stats=FAKE, grad=FAKE, ldg=100, ws=FAKE, ws_bytes=1 << 30, stream=None)
+    args.update(over)
+    return args
+
+
+@pytest.mark.parametrize("over,needle", [
+    (dict(rows=-1), "rows"), (dict(V=0), "V"), (dict(dtype=3), "dtype"),
+    (dict(tdtype=-1), "teacher_dtype"), (dict(K=-1), "K"), (dict(K=1025), "K"),
+    (dict(T=0.0), "temperature"), (dict(T=float("nan")), "temperature"),
+    (dict(T=2.0**21), "temperature"), (dict(soft=float("inf")), "soft"),
+    (dict(hard=float("nan")), "hard"), (dict(ids=None), "ids"),
+    (dict(teacher=None), "teacher"), (dict(ids=FAKE + 2), "ids"),
+    (dict(logits=None), "logits"), (dict(ld=99), "logits"), (dict(loss=None), "loss"),
+    (dict(stats=None), "stats"), (dict(ldg=99), "grad"), (dict(labels=FAKE + 1), "labels"),
+    (dict(weight=FAKE + 1), "row_weight"), (dict(ws=None), "workspace"),
+    (dict(ws=FAKE + 8), "aligned"), (dict(ld=120, ldg=110, grad=FAKE), "stride"),
+])
+def test_distill_rejects(over, needle):
+    refused(w2v.lib().w2v_distill_loss, distill_args(**over), needle)
+
+
+@pytest.mark.parametrize("over,needle", [
+    (dict(rows=-1), "rows"), (dict(K=1025), "K"), (dict(T=-1.0), "temperature"),
+    (dict(dloss=None), "dloss"), (dict(stats=None), "stats"), (dict(grad=None), "grad"),
+    (dict(grad=FAKE, ldg=101), "stride"), (dict(logits=None), "logits"),
+])
+def test_distill_backward_rejects(over, needle):
+    args = dict(dloss=FAKE, logits=FAKE, ld=100, rows=4, V=100, dtype=0, ids=FAKE,
+                teacher=FAKE, K=8, tdtype=0, labels=None, T=2.0, soft=1.0, hard=0.0,
+                stats=FAKE, grad=FAKE, ldg=100, stream=None)
+    args.update(over)
+    refused(w2v.lib().w2v_distill_backward, args, needle)
+
+
+@pytest.mark.parametrize("over,needle,code", [
+    (dict(rows=-1), "rows", -1), (dict(V=0), "V", -1), (dict(dtype=5), "dtype", -1),
+    (dict(z=None), "logits", -1), (dict(ld=99), "logits", -1), (dict(u=None), "uniforms", -1),
+    (dict(ldu=99), "uniforms", -1), (dict(T=-1.0), "temperature", -1),
+    (dict(T=float("inf")), "temperature", -1), (dict(k=-1), "top_k", -1),
+    (dict(V=5000, ld=5000, ldu=5000, k=1025), "top_k", -4), (dict(p=0.0), "top_p", -1),
+    (dict(p=float("nan")), "top_p", -1), (dict(least=-0.1), "min_p", -1),
+    (dict(least=1.1), "min_p", -1), (dict(ids=None), "ids", -1), (dict(ts=FAKE + 1),
+                                                                "temperatures", -1),
+    (dict(lp=FAKE + 2), "logprob", -1), (dict(ws=None), "workspace", -1),
+    (dict(ws_bytes=10), "workspace", -1), (dict(ws=FAKE + 8), "aligned", -1),
+])
+def test_sample_rejects(over, needle, code):
+    args = dict(z=FAKE, ld=100, u=FAKE, ldu=100, rows=4, V=100, dtype=0, ts=None, T=1.0,
+                ks=None, k=0, ps=None, p=1.0, ms=None, least=0.0, ids=FAKE, lp=None, ws=FAKE,
+                ws_bytes=1 << 30, stream=None)
+    args.update(over)
+    refused(w2v.lib().w2v_sample_words, args, needle, code)
