@@ -19,7 +19,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 HIP_SOURCES = ["api.hip", "epoch_kernels.hip", "pairwise_kernels.hip",
                "step_kernels.hip", "step_sorted.hip", "vocab.hip", "radix_sort.hip",
-               "head_api.hip", "linear.hip", "distill.hip", "sample.hip"]
+               "head_api.hip", "linear.hip", "linear_f32.hip", "linear_bf16.hip",
+               "linear_f16.hip", "distill.hip", "sample.hip"]
 CXX_SOURCES = ["tables.cpp"]
 
 HIP_FLAGS = [

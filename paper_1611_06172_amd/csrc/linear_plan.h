@@ -1,0 +1,106 @@
+// How the vocabulary head's matrix products are cut into tiles, splits and
+// workspace (host only).
+#pragma once
+
+#include "linear.h"
+#include "w2v.h"
+
+namespace w2v {
+
+// Output tiles, and 16-byte granules of k per tile row in LDS.
+struct Tile {
+  int rows, cols, granules;
+};
+constexpr Tile kTiles[3] = {{64, 64, 8}, {128, 64, 4}, {128, 128, 4}};
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
+inline int element_size(int32_t dtype) { return dtype == W2V_DTYPE_F32 ? 4 : 2; }
+
+// Tile and split of a product.
+struct Plan {
+  int32_t tile;  // of kTiles
+  int32_t tiles_m, tiles_n, splits, k_per_split;
+};
+
+// Blocks that the GPU holds at once, 4 on each of 256 CUs.
+constexpr int kSlots = 1024;
+
+// The tile whose padded output costs least. What a tile's element costs beside
+// one of a 128 x 128 tile, by products that fill the GPU (8192 x 8192 outputs,
+// k 2048): fp32, bound by MFMA, 1.10 for 64 x 64 and 1.07 for 128 x 64; 16 bits,
+// bound by LDS reads, 1.8 and 1.45, but 1.35 and 1.15 where both operands are
+// turned (dW). An output with fewer tiles than the GPU holds blocks leaves
+// that share of it idle: bf16 65,536 x 300 x 300 takes 42 us with 128 x 128
+// tiles and 51 with 64 x 64 ones, 4,096 x 600 x 600 29 and 17.
+// A product with a long k and few tiles is split along k into as many blocks
+// as the GPU holds, of at least 8 tiles of k each.
+inline Plan plan_product(int32_t M, int32_t N, int32_t K, int32_t dtype, bool both_turned) {
+  static const double kCost[3][3] = {{1.10, 1.07, 1.0}, {1.8, 1.45, 1.0}, {1.35, 1.15, 1.0}};
+  const double* cost = kCost[dtype == W2V_DTYPE_F32 ? 0 : both_turned ? 2 : 1];
+  Plan best{};
+  double least = 0.0;
+  for (int i = 2; i >= 0; i--) {
+    const Tile& t = kTiles[i];
+    Plan p;
+    p.tile = i;
+    p.tiles_m = (int32_t)ceil_div(M, t.rows);
+    p.tiles_n = (int32_t)ceil_div(N, t.cols);
+    const int64_t k_tiles = ceil_div(K, t.granules * 16 / element_size(dtype));
+    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+    int64_t splits = kSlots / tiles;
+    if (splits > k_tiles / 8) splits = k_tiles / 8;
+    if (splits > 64) splits = 64;
+    if (splits < 1) splits = 1;
+    p.k_per_split = (int32_t)ceil_div(k_tiles, splits);
+    p.splits = (int32_t)ceil_div(k_tiles, p.k_per_split);
+    const double blocks = (double)tiles * p.splits;
+    double c = cost[i] * (double)tiles * t.rows * t.cols;
+    if (blocks < kSlots) c *= kSlots / blocks;
+    if (i == 2 || c < least) {
+      best = p;
+      least = c;
+    }
+  }
+  return best;
+}
+
+inline size_t partial_bytes(const Plan& p, int32_t M, int32_t N) {
+  return p.splits == 1 ? 0 : aligned((size_t)p.splits * M * N * 4);
+}
+
+// Rows of x up to which W is streamed past them (k_few_rows).
+constexpr int kFewRows = 32;
+
+inline bool few_rows(int32_t M, int32_t K) { return M <= kFewRows && K <= 8192; }
+
+// The backward pass's parts of its workspace.
+struct BackwardPlan {
+  Plan dx, dw;
+  size_t dz, partial, sums;  // bytes
+};
+
+inline BackwardPlan plan_backward(int32_t M, int32_t N, int32_t K, int32_t dtype,
+                                  int32_t activation) {
+  BackwardPlan b{};
+  if (M == 0) return b;
+  b.dx = plan_product(M, K, N, dtype, false);
+  b.dw = plan_product(N, K, M, dtype, true);
+  b.dz = activation == W2V_ACTIVATION_NONE
+             ? 0
+             : aligned((size_t)M * N * element_size(dtype));
+  const size_t px = partial_bytes(b.dx, M, K), pw = partial_bytes(b.dw, N, K);
+  b.partial = px > pw ? px : pw;
+  b.sums = b.dw.splits == 1 ? 0 : aligned((size_t)b.dw.splits * N * 4);
+  return b;
+}
+
+// One element type's launches (linear_<type>.hip).
+hipError_t launch_linear_f32(const LinearArgs& l, void* workspace, hipStream_t s);
+hipError_t launch_linear_bf16(const LinearArgs& l, void* workspace, hipStream_t s);
+hipError_t launch_linear_f16(const LinearArgs& l, void* workspace, hipStream_t s);
+hipError_t launch_backward_f32(const LinearBackwardArgs& l, void* workspace, hipStream_t s);
+hipError_t launch_backward_bf16(const LinearBackwardArgs& l, void* workspace, hipStream_t s);
+hipError_t launch_backward_f16(const LinearBackwardArgs& l, void* workspace, hipStream_t s);
+
+}  // namespace w2v
