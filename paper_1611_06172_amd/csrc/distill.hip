@@ -15,17 +15,15 @@ namespace w2v {
 namespace {
 
 constexpr int kThreads = 512;
-constexpr int kMaxList = W2V_MAX_TEACHER;
 
 // How p_1 is formed beside p_T.
-constexpr int kSoftOnly = 0;  // not at all: no row has a label
-constexpr int kPower = 1;     // T = 2^n: exp(x) is exp(x / T) squared n times
-constexpr int kBoth = 2;      // any T: an exponential of its own
+constexpr int kSoftOnly = -1;  // not at all: no row has a label
+// 0, 1, 2: T is 1, 2 or 4, and exp(x) is exp(x / T) squared that often
+constexpr int kBoth = 3;  // any T: an exponential of its own
 
 struct Ctx {
   DistillArgs a;
   float scale;    // log2(e) / T
-  int squarings;  // n of kPower
   int splits;     // of a row
   int64_t range;  // elements of a split
   float* parts;   // [rows][splits][3]
@@ -51,22 +49,17 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float scale) {
   return o;
 }
 
-__device__ __forceinline__ float squared(float e, int squarings) {
-  for (int i = 0; i < squarings; i++) e *= e;
-  return e;
-}
-
+// exp(d) beside e = exp(d / T).
 template <int MODE>
-__device__ __forceinline__ float hard_of(float d, float e, int squarings) {
-  if constexpr (MODE == kPower) return squared(e, squarings);
+__device__ __forceinline__ float hard_of(float d, float e) {
   if constexpr (MODE == kBoth) return exp2_fast(d * kLog2e);
-  return 0.0f;
+  for (int i = 0; i < MODE; i++) e *= e;
+  return e;
 }
 
 // Adds N scores. The maximum is moved once for all of them.
 template <int MODE, int N>
-__device__ __forceinline__ void add(Sums& s, const float (&v)[N], float scale,
-                                    int squarings) {
+__device__ __forceinline__ void add(Sums& s, const float (&v)[N], float scale) {
   float m = v[0];
 #pragma unroll
   for (int i = 1; i < N; i++) m = fmaxf(m, v[i]);
@@ -82,66 +75,94 @@ __device__ __forceinline__ void add(Sums& s, const float (&v)[N], float scale,
     const float d = v[i] - base;
     const float e = exp2_fast(d * scale);
     soft += e;
-    if constexpr (MODE != kSoftOnly) hard += hard_of<MODE>(d, e, squarings);
+    if constexpr (MODE != kSoftOnly) hard += hard_of<MODE>(d, e);
   }
   s.soft += soft;
   s.hard += hard;
 }
 
-// The sums over the block's share [lo, hi) of a row, in every thread.
-template <typename T, int MODE>
-__device__ Sums scan(const T* row, int64_t lo, int64_t hi, const Ctx& c, float* scratch) {
-  constexpr int N = 16 / (int)sizeof(T);
+// The elements of 16 bytes, taken from whole words: the pack stays in four
+// registers.
+template <typename T>
+__device__ __forceinline__ void unpack_words(uint4 w, float (&out)[16 / (int)sizeof(T)]) {
+  const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    if constexpr (sizeof(T) == 4) {
+      out[i] = __builtin_bit_cast(float, word[i]);
+    } else {
+      const uint16_t lo = (uint16_t)word[i], hi = (uint16_t)(word[i] >> 16);
+      out[2 * i] = to_f32(__builtin_bit_cast(T, lo));
+      out[2 * i + 1] = to_f32(__builtin_bit_cast(T, hi));
+    }
+  }
+}
+
+// The thread's share of the sums over [lo, hi) of a row.
+template <typename T, int MODE, int THREADS>
+__device__ __forceinline__ Sums scan(const T* row, int64_t lo, int64_t hi, const Ctx& c) {
+  constexpr int N = 16 / (int)sizeof(T), U = 4;
   const int tid = threadIdx.x;
   Sums s = {-INFINITY, 0.0f, 0.0f};
   const int64_t packs = (hi - lo) / N;
-  constexpr int U = 4;
   int64_t p = tid;
-  for (; p + (U - 1) * kThreads < packs; p += U * kThreads) {
-    Pack<T, N> in[U];
+  for (; p + (U - 1) * THREADS < packs; p += U * THREADS) {
+    uint4 in[U];
 #pragma unroll
-    for (int u = 0; u < U; u++) in[u] = load_pack<T, N>(row + lo + (p + u * kThreads) * N);
+    for (int u = 0; u < U; u++) in[u] = load_16(row + lo + (p + u * THREADS) * N);
 #pragma unroll
     for (int u = 0; u < U; u++) {
       float v[N];
-#pragma unroll
-      for (int i = 0; i < N; i++) v[i] = to_f32(in[u].v[i]);
-      add<MODE, N>(s, v, c.scale, c.squarings);
+      unpack_words<T>(in[u], v);
+      add<MODE, N>(s, v, c.scale);
     }
   }
-  for (; p < packs; p += kThreads) {
-    const Pack<T, N> in = load_pack<T, N>(row + lo + p * N);
+  for (; p < packs; p += THREADS) {
     float v[N];
-#pragma unroll
-    for (int i = 0; i < N; i++) v[i] = to_f32(in.v[i]);
-    add<MODE, N>(s, v, c.scale, c.squarings);
+    unpack_words<T>(load_16(row + lo + p * N), v);
+    add<MODE, N>(s, v, c.scale);
   }
   if (lo + packs * N + tid < hi) {
     const float v[1] = {to_f32(row[lo + packs * N + tid])};
-    add<MODE, 1>(s, v, c.scale, c.squarings);
+    add<MODE, 1>(s, v, c.scale);
   }
-  const float m = block_max(s.max, scratch);
-  s.soft *= rescale(s.max, m, c.scale);
-  s.hard *= rescale(s.max, m, kLog2e);
-  s.max = m;
-  s.soft = block_sum(s.soft, scratch);
-  if constexpr (MODE != kSoftOnly) s.hard = block_sum(s.hard, scratch);
   return s;
 }
 
-// The teacher's list of a row, in LDS: q of each entry (0 where absent).
+// The block's sums from its threads', relative to the maximum m.
+template <int MODE>
+__device__ __forceinline__ Sums block_of(Sums s, float m, const Ctx& c, float* scratch) {
+  s.soft *= rescale(s.max, m, c.scale);
+  if constexpr (MODE == kSoftOnly) {
+    s.soft = block_sum(s.soft, scratch);
+  } else {
+    s.hard *= rescale(s.max, m, kLog2e);
+    block_sums(s.soft, s.hard, scratch);
+  }
+  s.max = m;
+  return s;
+}
+
+// The teacher's list of a row in LDS, and its label as one more entry: the
+// word (-1: absent), the teacher's logit (then what is taken from the entry's
+// gradient) and the student's score.
 struct List {
-  int32_t id[kMaxList + 1];
-  float q[kMaxList + 1];  // then what is taken from the entry's gradient
-  float s[kMaxList + 1];  // the student's score
-  float scratch[16];
-  int bad;
+  int32_t* id;
+  float* q;
+  float* s;
+  float* scratch;  // 32
 };
+__device__ __forceinline__ List list_of(const Ctx& c) {
+  extern __shared__ float memory[];
+  const int n = c.a.K + 1;
+  return List{(int32_t*)(memory + 32), memory + 32 + n, memory + 32 + 2 * n, memory};
+}
 
 struct Row {
   bool some;       // lists a word
   bool ok;         // every id is a word or -1
   int32_t label;   // or -1
+  float weight;    // of the gradient
   float max, log;  // of the list's t / T: q_k = exp(t_k / T - max - log)
 };
 
@@ -160,39 +181,37 @@ __device__ __forceinline__ float teacher_logit(const Ctx& c, int row, int k) {
   }
 }
 
-// Reads the row's list and its label; q sums to 1 over the present entries.
-// t - max comes first, so that any finite t / T is within range.
-__device__ Row read_list(const Ctx& c, int row, List& l) {
+// Reads the row's list and its label with the student's scores of their words;
+// q sums to 1 over the present entries. t - max comes first, so that any finite
+// t / T is within range.
+template <typename T>
+__device__ __forceinline__ Row read_list(const Ctx& c, int row, const List& l) {
   const int tid = threadIdx.x, step = blockDim.x;
+  const T* logits = (const T*)c.a.logits + row * c.a.ld;
   Row r;
-  if (tid == 0) l.bad = 0;
   r.label = c.a.labels == nullptr ? -1 : c.a.labels[row];
-  __syncthreads();
-  float m = -INFINITY;
-  bool bad = r.label < -1 || r.label >= c.a.V;
-  for (int k = tid; k < c.a.K; k += step) {
-    const int32_t id = c.a.ids[(int64_t)row * c.a.K + k];
-    bad |= id < -1 || id >= c.a.V;
-    const float t = id < 0 ? -INFINITY : teacher_logit(c, row, k);
+  r.weight = c.a.row_weight == nullptr ? 1.0f : c.a.row_weight[row];
+  float m = -INFINITY, fault = 0.0f;  // 1: NaN, which the row's loss shows; 2: an id
+  for (int k = tid; k <= c.a.K; k += step) {
+    const int32_t id = k == c.a.K ? r.label : c.a.ids[(int64_t)row * c.a.K + k];
+    const bool word = id >= 0 && id < c.a.V;
+    const float t = k == c.a.K || !word ? -INFINITY : teacher_logit(c, row, k);
     l.id[k] = id;
     l.q[k] = t;
-    m = t > m || t != t ? t : m;  // NaN is kept: the row's loss shows it
+    l.s[k] = word ? to_f32(logits[id]) : 0.0f;
+    m = fmaxf(m, t);
+    fault = fmaxf(fault, id < -1 || id >= c.a.V ? 2.0f : t != t ? 1.0f : 0.0f);
   }
-  if (bad) l.bad = 1;
-  const float seen = block_sum(m != m ? 1.0f : 0.0f, l.scratch);
-  m = block_max(m, l.scratch);
-  if (seen > 0.0f) m = NAN;
-  r.ok = l.bad == 0;
+  block_maxima(m, fault, l.scratch);
+  if (fault == 1.0f) m = NAN;
+  r.ok = fault < 2.0f;
   r.some = m != -INFINITY;
   r.max = m;
   float sum = 0.0f;
-  for (int k = tid; k < c.a.K; k += step) {
-    const float e = r.some && l.id[k] >= 0 ? expf((l.q[k] - m) / c.a.temperature) : 0.0f;
-    sum += e;
-  }
+  for (int k = tid; k < c.a.K; k += step)
+    sum += r.some && l.id[k] >= 0 ? expf((l.q[k] - m) / c.a.temperature) : 0.0f;
   sum = block_sum(sum, l.scratch);
   r.log = r.some ? logf(sum) : 0.0f;
-  __syncthreads();
   return r;
 }
 
@@ -203,11 +222,12 @@ __device__ __forceinline__ float log_q(const Ctx& c, const Row& r, float t) {
 
 template <typename T, int MODE>
 __global__ __launch_bounds__(kThreads) void k_sums(Ctx c) {
-  __shared__ float scratch[16];
+  __shared__ float scratch[32];
   const int row = blockIdx.x / c.splits, split = blockIdx.x % c.splits;
   const int64_t lo = split * c.range;
   const int64_t hi = lo + c.range < c.a.V ? lo + c.range : c.a.V;
-  const Sums s = scan<T, MODE>((const T*)c.a.logits + row * c.a.ld, lo, hi, c, scratch);
+  Sums s = scan<T, MODE, kThreads>((const T*)c.a.logits + row * c.a.ld, lo, hi, c);
+  s = block_of<MODE>(s, block_max(s.max, scratch), c, scratch);
   if (threadIdx.x == 0) {
     float* out = c.parts + ((int64_t)row * c.splits + split) * 3;
     out[0] = s.max;
@@ -217,10 +237,8 @@ __global__ __launch_bounds__(kThreads) void k_sums(Ctx c) {
 }
 
 // A row's loss from its sums (every thread has them); thread 0 writes it.
-template <typename T>
-__device__ void write_loss(const Ctx& c, int row, const Row& r, const List& l, const Sums& s,
-                           float* scratch) {
-  const T* logits = (const T*)c.a.logits + row * c.a.ld;
+__device__ __forceinline__ void write_loss(const Ctx& c, int row, const Row& r, const List& l,
+                                           const Sums& s) {
   const float log_soft = logf(s.soft), log_hard = s.hard > 0.0f ? logf(s.hard) : 0.0f;
   const bool live = r.ok && log_soft != -INFINITY;  // some score is above -inf
   float v = 0.0f;
@@ -229,15 +247,13 @@ __device__ void write_loss(const Ctx& c, int row, const Row& r, const List& l, c
       if (l.id[k] < 0) continue;
       const float lq = log_q(c, r, l.q[k]), q = expf(lq);
       if (q == 0.0f) continue;
-      const float x = (to_f32(logits[l.id[k]]) - s.max) / c.a.temperature;
-      v += q * (lq - (x - log_soft));
+      v += q * (lq - ((l.s[k] - s.max) / c.a.temperature - log_soft));
     }
   }
-  v = block_sum(v, scratch);
+  v = block_sum(v, l.scratch);
   if (threadIdx.x == 0) {
     float loss = c.a.soft * c.a.temperature * c.a.temperature * v;
-    if (live && r.label >= 0)
-      loss += c.a.hard * (log_hard - (to_f32(logits[r.label]) - s.max));
+    if (live && r.label >= 0) loss += c.a.hard * (log_hard - (l.s[c.a.K] - s.max));
     if (!live) loss = 0.0f;
     c.a.loss[row] = loss;
     c.a.stats[(int64_t)row * 3] = s.max;
@@ -249,56 +265,70 @@ __device__ void write_loss(const Ctx& c, int row, const Row& r, const List& l, c
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_loss(Ctx c) {
-  __shared__ List l;
+  const List l = list_of(c);
   const int row = blockIdx.x;
-  const Row r = read_list(c, row, l);
+  const Row r = read_list<T>(c, row, l);
   Sums s = {-INFINITY, 0.0f, 0.0f};
   for (int i = 0; i < c.splits; i++) {
     const float* in = c.parts + ((int64_t)row * c.splits + i) * 3;
     s = join(s, Sums{in[0], in[1], in[2]}, c.scale);
   }
-  write_loss<T>(c, row, r, l, s, l.scratch);
+  write_loss(c, row, r, l, s);
 }
 
 // What a row's gradient is made of: soft p_T + hard p_1 from the statistics,
 // less the amounts of the listed words and the label.
 struct Slope {
-  float max, soft, hard;  // exp2((s - max) scale) soft + exp2((s - max) log2e) hard
+  float max, soft, hard;  // exp((s - max) / T) soft + exp(s - max) hard
+  bool none;              // the row's gradient is 0
 };
 
 template <int MODE>
 __device__ __forceinline__ float slope_at(const Slope& g, float s, const Ctx& c) {
   const float d = s - g.max, e = exp2_fast(d * c.scale);
-  float v = g.soft * e;
-  if constexpr (MODE != kSoftOnly) v += g.hard * hard_of<MODE>(d, e, c.squarings);
-  return v;
+  if constexpr (MODE == kSoftOnly) return g.soft * e;
+  if constexpr (MODE == 0) return (g.soft + g.hard) * e;
+  if constexpr (MODE == 1) return __builtin_fmaf(g.hard, e, g.soft) * e;
+  return g.soft * e + g.hard * hard_of<MODE>(d, e);
 }
 
-// Turns the list into the entries of the gradient within [lo, hi): the
-// student's score (read before the gradient may overwrite it) and the amount
-// to take off; the label is one more entry.
-template <typename T>
-__device__ Slope begin_gradient(const Ctx& c, int row, const Row& r, List& l, float max,
-                                float log_soft, float log_hard, int64_t lo, int64_t hi) {
-  const T* logits = (const T*)c.a.logits + row * c.a.ld;
-  const float w = c.a.row_weight == nullptr ? 1.0f : c.a.row_weight[row];
-  const float soft = w * c.a.soft * c.a.temperature, hard = w * c.a.hard;
+// The gradient's N elements from the scores.
+template <typename T, int MODE, int N>
+__device__ __forceinline__ Pack<T, N> slopes(const Slope& g, const float (&v)[N],
+                                             const Ctx& c) {
+  Pack<T, N> o;
+  if (g.none) {  // uniform over the block
+#pragma unroll
+    for (int j = 0; j < N; j++) o.v[j] = T(0.0f);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; j++) o.v[j] = from_f32<T>(slope_at<MODE>(g, v[j], c));
+  }
+  return o;
+}
+
+// Turns the list into the entries of the gradient within [lo, hi): the amount
+// to take off. The student's scores were read before the gradient may overwrite
+// them.
+__device__ __forceinline__ Slope begin_gradient(const Ctx& c, const Row& r, const List& l,
+                                                float max, float log_soft, float log_hard,
+                                                int64_t lo, int64_t hi) {
+  const float soft = r.weight * c.a.soft * c.a.temperature, hard = r.weight * c.a.hard;
   const bool live = r.ok && log_soft != -INFINITY;
   for (int k = threadIdx.x; k <= c.a.K; k += blockDim.x) {
-    if (k == c.a.K) {
-      l.id[k] = r.label;
-      l.q[k] = hard;
-    } else {
-      l.q[k] = l.id[k] < 0 ? 0.0f : soft * expf(log_q(c, r, l.q[k]));
-    }
+    l.q[k] = k == c.a.K ? hard : l.id[k] < 0 ? 0.0f : soft * expf(log_q(c, r, l.q[k]));
     if (!live || l.id[k] < lo || l.id[k] >= hi) l.id[k] = -1;
-    if (l.id[k] >= 0) l.s[k] = to_f32(logits[l.id[k]]);
   }
   __syncthreads();
-  Slope g = {max, 0.0f, 0.0f};
-  if (live && r.some) g.soft = soft * expf(-log_soft);
-  if (live && r.label >= 0) g.hard = hard * expf(-log_hard);
-  if (!live) g.max = 0.0f;
+  Slope g = {max, 0.0f, 0.0f, true};
+  if (live && r.some) {
+    g.soft = soft * expf(-log_soft);
+    g.none = false;
+  }
+  if (live && r.label >= 0) {
+    g.hard = hard * expf(-log_hard);
+    g.none = false;
+  }
   return g;
 }
 
@@ -317,36 +347,164 @@ __device__ void end_gradient(const Ctx& c, int row, const List& l, const Slope& 
 
 template <typename T, int MODE>
 __global__ __launch_bounds__(kThreads) void k_gradient(Ctx c) {
-  __shared__ List l;
+  const List l = list_of(c);
   constexpr int N = 16 / (int)sizeof(T);
   const int row = blockIdx.x / c.splits, split = blockIdx.x % c.splits, tid = threadIdx.x;
   const int64_t lo = split * c.range;
   const int64_t hi = lo + c.range < c.a.V ? lo + c.range : c.a.V;
-  const Row r = read_list(c, row, l);
+  const Row r = read_list<T>(c, row, l);
   if (!r.ok && tid == 0)
     __hip_atomic_store(c.a.status, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
   const float* stats = c.a.stats + (int64_t)row * 3;
-  const Slope g = begin_gradient<T>(c, row, r, l, stats[0], stats[1], stats[2], lo, hi);
-  const bool none = g.soft == 0.0f && g.hard == 0.0f;
+  const Slope g = begin_gradient(c, r, l, stats[0], stats[1], stats[2], lo, hi);
   const T* in = (const T*)c.a.logits + row * c.a.ld;
   T* out = (T*)c.a.grad + row * c.a.ldg;
   const int64_t packs = (hi - lo) / N;
   for (int64_t p = tid; p < packs; p += kThreads) {
     const int64_t at = lo + p * N;
-    const Pack<T, N> v = load_pack<T, N>(in + at);
-    Pack<T, N> o;
-#pragma unroll
-    for (int i = 0; i < N; i++)
-      o.v[i] = from_f32<T>(none ? 0.0f : slope_at<MODE>(g, to_f32(v.v[i]), c));
-    store_pack<T, N>(out + at, o);
+    float v[N];
+    unpack_words<T>(load_16(in + at), v);
+    store_pack<T, N>(out + at, slopes<T, MODE>(g, v, c));
   }
   const int64_t last = lo + packs * N + tid;
-  if (last < hi) out[last] = from_f32<T>(none ? 0.0f : slope_at<MODE>(g, to_f32(in[last]), c));
+  if (last < hi) {
+    const float v[1] = {to_f32(in[last])};
+    out[last] = slopes<T, MODE>(g, v, c).v[0];
+  }
   __syncthreads();
   end_gradient<T, MODE>(c, row, l, g);
 }
 
+// Keeps the compiler from carrying a pack's elements in unpacked form past this
+// point, at twice the registers.
+__device__ __forceinline__ void keep_packed(uint4& v) {
+  asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w));
+}
+
+// Elements at .. at + N - 1 of a row of V, those past its end -inf, in 16 bytes.
+template <typename T, int N>
+__device__ __forceinline__ uint4 load_filled(const T* row, int64_t at, int64_t V) {
+  typedef unsigned __int128 u128;
+  constexpr int kBits = 8 * (int)sizeof(T);
+  if (at + N <= V) return load_16(row + at);
+  const T low = T(-INFINITY);
+  u128 one = 0;
+  __builtin_memcpy(&one, &low, sizeof(T));
+  u128 fill = 0;
+#pragma unroll
+  for (int i = 0; i < N; i++) fill = fill << kBits | one;
+  if (at >= V) return __builtin_bit_cast(uint4, fill);
+  const int n = (int)(V - at);  // elements there are
+  if (V >= N) {  // the last N elements, moved down
+    const u128 v = __builtin_bit_cast(u128, load_16(row + V - N));
+    return __builtin_bit_cast(uint4, v >> ((N - n) * kBits) | fill << (n * kBits));
+  }
+  u128 v = fill << (n * kBits);
+  for (int i = 0; i < n; i++) {
+    u128 e = 0;
+    const T x = row[at + i];
+    __builtin_memcpy(&e, &x, sizeof(T));
+    v |= e << (i * kBits);
+  }
+  return __builtin_bit_cast(uint4, v);
+}
+
+// Loss and gradient of a row by one block. The end of the row stays in
+// registers, NV packs of 16 bytes a thread, between the sums and the gradient;
+// STREAM: of longer rows the first part is read twice, the second time
+// backwards, from what was read last.
+template <typename T, int MODE, int THREADS, int NV, bool STREAM>
+__global__ __launch_bounds__(THREADS) void k_row(Ctx c) {
+  const List l = list_of(c);
+  constexpr int N = 16 / (int)sizeof(T);
+  const int tid = threadIdx.x;
+  const int64_t V = c.a.V;
+  // what is read twice: whole turns of the block
+  const int64_t over = V - (int64_t)THREADS * NV * N;
+  const int64_t head =
+      STREAM && over > 0 ? (over + THREADS * N - 1) / (THREADS * N) * (THREADS * N) : 0;
+  uint4 kept[NV];
+  const int64_t row = blockIdx.x;
+  const T* in = (const T*)c.a.logits + row * c.a.ld;
+#pragma unroll
+  for (int i = 0; i < NV; i++)
+    kept[i] = load_filled<T, N>(in, head + (tid + i * THREADS) * (int64_t)N, V);
+  const Row r = read_list<T>(c, (int)row, l);
+  Sums s = {-INFINITY, 0.0f, 0.0f};
+  if (STREAM) s = scan<T, MODE, THREADS>(in, 0, head, c);
+  float m = s.max;
+#pragma unroll
+  for (int i = 0; i < NV; i++) {
+    float v[N];
+    unpack_words<T>(kept[i], v);
+#pragma unroll
+    for (int j = 0; j < N; j++) m = fmaxf(m, v[j]);
+    keep_packed(kept[i]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  m = block_max(m, l.scratch);
+  s.soft *= rescale(s.max, m, c.scale);
+  s.hard *= rescale(s.max, m, kLog2e);
+  s.max = m;
+  const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+  for (int i = 0; i < NV; i++) {
+    float soft = 0.0f, hard = 0.0f, v[N];
+    unpack_words<T>(kept[i], v);
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+      const float d = v[j] - base, e = exp2_fast(d * c.scale);
+      soft += e;
+      if constexpr (MODE != kSoftOnly) hard += hard_of<MODE>(d, e);
+    }
+    s.soft += soft;
+    s.hard += hard;
+    keep_packed(kept[i]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  s = block_of<MODE>(s, m, c, l.scratch);
+  write_loss(c, (int)row, r, l, s);
+  if (c.a.grad == nullptr) return;
+
+  const float log_soft = logf(s.soft), log_hard = s.hard > 0.0f ? logf(s.hard) : 0.0f;
+  const Slope g = begin_gradient(c, r, l, s.max, log_soft, log_hard, 0, V);
+  T* out = (T*)c.a.grad + row * c.a.ldg;
+#pragma unroll
+  for (int i = 0; i < NV; i++) {
+    const int64_t at = head + (tid + i * THREADS) * (int64_t)N;
+    float v[N];
+    unpack_words<T>(kept[i], v);
+    const Pack<T, N> o = slopes<T, MODE>(g, v, c);
+    if (at < V) store_some<T, N>(out + at, V - at, o);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (STREAM) {
+    constexpr int U = 4;
+    int64_t turn = head / (THREADS * N);
+    while (turn > 0) {
+      const int n = turn < U ? (int)turn : U;
+      turn -= n;
+      uint4 w[U];
+#pragma unroll
+      for (int u = 0; u < U; u++)
+        if (u < n) w[u] = load_16(in + ((turn + u) * THREADS + tid) * (int64_t)N);
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        if (u >= n) break;
+        float v[N];
+        unpack_words<T>(w[u], v);
+        store_pack<T, N>(out + ((turn + u) * THREADS + tid) * (int64_t)N,
+                         slopes<T, MODE>(g, v, c));
+      }
+    }
+  }
+  __syncthreads();
+  end_gradient<T, MODE>(c, (int)row, l, g);
+}
+
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+constexpr int kCUs = 256;
 
 // Blocks of a row: enough for the GPU to be full with few rows, each with at
 // least 8192 elements.
@@ -361,7 +519,6 @@ Ctx context(const DistillArgs& a) {
   Ctx c{};
   c.a = a;
   c.scale = kLog2e / a.temperature;
-  c.squarings = a.temperature == 1.0f ? 0 : a.temperature == 2.0f ? 1 : 2;
   c.splits = splits_of(a.rows, a.V);
   c.range = ceil_div(ceil_div(a.V, c.splits), 64) * 64;
   c.splits = (int)ceil_div(a.V, c.range);
@@ -370,12 +527,27 @@ Ctx context(const DistillArgs& a) {
 
 template <typename T, int MODE>
 hipError_t launch_as(const Ctx& c, bool forward, hipStream_t s) {
-  const int grid = c.a.rows * c.splits;
-  if (forward) {
-    k_sums<T, MODE><<<grid, kThreads, 0, s>>>(c);
-    k_loss<T><<<c.a.rows, kThreads, 0, s>>>(c);
+  constexpr int N = 16 / (int)sizeof(T);
+  const int rows = c.a.rows, V = c.a.V;
+  const size_t lds = 32 * 4 + (size_t)(c.a.K + 1) * 12;
+  if (forward && V <= 64 * 4 * N && c.a.K <= 128) {
+    k_row<T, MODE, 64, 4, false><<<rows, 64, lds, s>>>(c);
+  } else if (forward && V <= 256 * 4 * N) {
+    k_row<T, MODE, 256, 4, false><<<rows, 256, lds, s>>>(c);
+  } else if (forward && V <= 512 * 9 * N) {
+    k_row<T, MODE, 512, 9, false><<<rows, 512, lds, s>>>(c);
+  } else if (forward && V <= 512 * 18 * N) {
+    k_row<T, MODE, 512, 18, false><<<rows, 512, lds, s>>>(c);
+  } else if (forward && (V <= 1024 * 14 * N || rows >= kCUs)) {
+    k_row<T, MODE, 1024, 14, true><<<rows, 1024, lds, s>>>(c);
+  } else {
+    const int grid = rows * c.splits;
+    if (forward) {
+      k_sums<T, MODE><<<grid, kThreads, 0, s>>>(c);
+      k_loss<T><<<rows, kThreads, lds, s>>>(c);
+    }
+    if (c.a.grad != nullptr) k_gradient<T, MODE><<<grid, kThreads, lds, s>>>(c);
   }
-  if (c.a.grad != nullptr) k_gradient<T, MODE><<<grid, kThreads, 0, s>>>(c);
   return hipGetLastError();
 }
 
@@ -383,7 +555,9 @@ template <typename T>
 hipError_t launch_type(const Ctx& c, bool forward, hipStream_t s) {
   if (c.a.labels == nullptr) return launch_as<T, kSoftOnly>(c, forward, s);
   const float t = c.a.temperature;
-  if (t == 1.0f || t == 2.0f || t == 4.0f) return launch_as<T, kPower>(c, forward, s);
+  if (t == 1.0f) return launch_as<T, 0>(c, forward, s);
+  if (t == 2.0f) return launch_as<T, 1>(c, forward, s);
+  if (t == 4.0f) return launch_as<T, 2>(c, forward, s);
   return launch_as<T, kBoth>(c, forward, s);
 }
 

@@ -44,6 +44,13 @@ __device__ __forceinline__ Pack<T, N> load_pack(const T* p) {
   return out;
 }
 
+// 16 bytes in four registers: elements that are only moved stay packed.
+__device__ __forceinline__ uint4 load_16(const void* p) {
+  uint4 v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+
 template <typename T, int N>
 __device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& v) {
   __builtin_memcpy(p, &v, sizeof(v));
@@ -146,6 +153,41 @@ __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
   return v;
+}
+// Two values at once; `scratch`: 32 floats.
+__device__ __forceinline__ void block_sums(float& a, float& b, float* scratch) {
+  a = wave_sum(a);
+  b = wave_sum(b);
+  const int w = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    scratch[w] = a;
+    scratch[16 + w] = b;
+  }
+  __syncthreads();
+  a = scratch[0];
+  b = scratch[16];
+  for (int i = 1; i < waves; i++) {
+    a += scratch[i];
+    b += scratch[16 + i];
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ void block_maxima(float& a, float& b, float* scratch) {
+  a = wave_max(a);
+  b = wave_max(b);
+  const int w = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    scratch[w] = a;
+    scratch[16 + w] = b;
+  }
+  __syncthreads();
+  a = scratch[0];
+  b = scratch[16];
+  for (int i = 1; i < waves; i++) {
+    a = fmaxf(a, scratch[i]);
+    b = fmaxf(b, scratch[16 + i]);
+  }
+  __syncthreads();
 }
 __device__ __forceinline__ float block_sum(float v, float* scratch) {
   v = wave_sum(v);
