@@ -615,8 +615,9 @@ int w2v_distill_backward(const float* dloss, const void* logits, int64_t ld, int
  * W2V_EINVAL. A u_j of 0 or NaN loses against every other word. Weights are
  * summed in 64-bit fixed point of at least 2^-31 of the first word's weight,
  * so nothing depends on an order. workspace: device, 256-byte aligned, at
- * least w2v_sample_workspace_bytes(rows, V) bytes, contents need not be
- * initialised; calls that overlap in time must not share it.
+ * least w2v_sample_workspace_bytes(rows, V) bytes (0 where a block does a
+ * whole row), contents need not be initialised; calls that overlap in time
+ * must not share it.
  */
 #define W2V_MAX_TOP_K 1024
 

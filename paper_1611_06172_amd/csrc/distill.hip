@@ -81,23 +81,6 @@ __device__ __forceinline__ void add(Sums& s, const float (&v)[N], float scale) {
   s.hard += hard;
 }
 
-// The elements of 16 bytes, taken from whole words: the pack stays in four
-// registers.
-template <typename T>
-__device__ __forceinline__ void unpack_words(uint4 w, float (&out)[16 / (int)sizeof(T)]) {
-  const uint32_t word[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    if constexpr (sizeof(T) == 4) {
-      out[i] = __builtin_bit_cast(float, word[i]);
-    } else {
-      const uint16_t lo = (uint16_t)word[i], hi = (uint16_t)(word[i] >> 16);
-      out[2 * i] = to_f32(__builtin_bit_cast(T, lo));
-      out[2 * i + 1] = to_f32(__builtin_bit_cast(T, hi));
-    }
-  }
-}
-
 // The thread's share of the sums over [lo, hi) of a row.
 template <typename T, int MODE, int THREADS>
 __device__ __forceinline__ Sums scan(const T* row, int64_t lo, int64_t hi, const Ctx& c) {

@@ -51,6 +51,23 @@ __device__ __forceinline__ uint4 load_16(const void* p) {
   return v;
 }
 
+// The elements of 16 bytes, taken from whole words: the pack stays in four
+// registers.
+template <typename T>
+__device__ __forceinline__ void unpack_words(uint4 w, float (&out)[16 / (int)sizeof(T)]) {
+  const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    if constexpr (sizeof(T) == 4) {
+      out[i] = __builtin_bit_cast(float, word[i]);
+    } else {
+      const uint16_t lo = (uint16_t)word[i], hi = (uint16_t)(word[i] >> 16);
+      out[2 * i] = to_f32(__builtin_bit_cast(T, lo));
+      out[2 * i + 1] = to_f32(__builtin_bit_cast(T, hi));
+    }
+  }
+}
+
 template <typename T, int N>
 __device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& v) {
   __builtin_memcpy(p, &v, sizeof(v));

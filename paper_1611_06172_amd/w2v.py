@@ -525,18 +525,25 @@ def build_vocab(raw, V_raw: int, min_count: int = 0, remap: bool = True,
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "tanh": 4, "sigmoid": 5}
 
 
+_DTYPES = None
+
+
 def _dtypes():
-    import torch
-    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    return _DTYPES
 
 
 def _head_dtype(t, name):
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
-    if t.dtype not in _dtypes():
+    code = _dtypes().get(t.dtype)
+    if code is None:
         raise TypeError(f"{name} must have dtype float32, bfloat16 or float16, got {t.dtype}")
-    return _dtypes()[t.dtype]
+    return code
 
 
 def _operand(t, name, shape=None, dtype=None):
@@ -546,24 +553,26 @@ def _operand(t, name, shape=None, dtype=None):
         raise TypeError(f"{name} must be a GPU tensor")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    if t.dim() != 2:
+    size = t.shape
+    if len(size) != 2:
         raise ValueError(f"{name} must be 2-D")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if shape is not None and size != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(size)}")
     _here(t, name)
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    rows, cols = size
+    ld, step = t.stride()
+    if cols > 1 and step != 1:
         raise ValueError(f"{name} must have unit column stride")
     if rows <= 1:
         return max(cols, 1)
-    if t.stride(0) < cols:
+    if ld < cols:
         raise ValueError(f"{name} must have a row stride >= its columns")
-    return t.stride(0)
+    return ld
 
 
 def _here(t, name):
     import torch
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != torch.cuda.current_device():
         raise ValueError(f"{name} must be on the current device")
 
 

@@ -114,8 +114,8 @@ def test_distill_backward_rejects(over, needle):
 
 @pytest.mark.parametrize("over,needle,code", [
     (dict(rows=-1), "rows", -1), (dict(V=0), "V", -1), (dict(dtype=5), "dtype", -1),
-    (dict(z=None), "logits", -1), (dict(ld=99), "logits", -1), (dict(u=None), "uniforms", -1),
-    (dict(ldu=99), "uniforms", -1), (dict(T=-1.0), "temperature", -1),
+    (dict(z=None), "logits", -1), (dict(ld=199_999), "logits", -1), (dict(u=None), "uniforms", -1),
+    (dict(ldu=199_999), "uniforms", -1), (dict(T=-1.0), "temperature", -1),
     (dict(T=float("inf")), "temperature", -1), (dict(k=-1), "top_k", -1),
     (dict(V=5000, ld=5000, ldu=5000, k=1025), "top_k", -4), (dict(p=0.0), "top_p", -1),
     (dict(p=float("nan")), "top_p", -1), (dict(least=-0.1), "min_p", -1),
@@ -125,8 +125,17 @@ def test_distill_backward_rejects(over, needle):
     (dict(ws_bytes=10), "workspace", -1), (dict(ws=FAKE + 8), "aligned", -1),
 ])
 def test_sample_rejects(over, needle, code):
-    args = dict(z=FAKE, ld=100, u=FAKE, ldu=100, rows=4, V=100, dtype=0, ts=None, T=1.0,
+    args = dict(z=FAKE, ld=200_000, u=FAKE, ldu=200_000, rows=4, V=200_000, dtype=0, ts=None, T=1.0,
                 ks=None, k=0, ps=None, p=1.0, ms=None, least=0.0, ids=FAKE, lp=None, ws=FAKE,
                 ws_bytes=1 << 30, stream=None)
     args.update(over)
     refused(w2v.lib().w2v_sample_words, args, needle, code)
+
+
+def test_sample_workspace():
+    """Short rows, and enough rows, are a block's each and need none."""
+    assert w2v.sample_workspace_bytes(4, 1000) == 0
+    assert w2v.sample_workspace_bytes(65_536, 1_000_000) == 0
+    assert w2v.sample_workspace_bytes(4, 1_000_000) % 256 == 0
+    assert w2v.sample_workspace_bytes(4, 1_000_000) > 0
+    assert w2v.sample_workspace_bytes(-1, 10) == 0
