@@ -84,15 +84,14 @@ __device__ __forceinline__ int granule_at(int r, int g) {
   return G == 8 ? r * 8 + (g ^ ((r ^ (r >> 3)) & 7)) : r * 4 + (g ^ (((r >> 1) ^ (r >> 3)) & 3));
 }
 
-// Elements k .. k + N - 1 of a row of K, those past its end 0. The granule
-// that the end cuts is read 16 bytes up to the end and moved down: no lane
-// waits for single elements.
+// N elements at `at`, of which the last `past` are beyond the end of a row of
+// `length` and become 0. They are read 16 bytes up to the end and moved down: no
+// lane waits for single elements.
 template <typename T, int N>
-__device__ __forceinline__ uint4 load_last(const T* row, int k, int K) {
-  if (K < N) return __builtin_bit_cast(uint4, load_some<T, N>(row + k, K - k));
-  const int past = k + N - K;  // elements past the end
+__device__ __forceinline__ uint4 load_end(const T* at, int past, int length) {
+  if (length < N) return __builtin_bit_cast(uint4, load_some<T, N>(at, N - past));
   typedef unsigned __int128 u128;
-  u128 v = __builtin_bit_cast(u128, load_pack<T, N>(row + (past > 0 ? K - N : k)));
+  u128 v = __builtin_bit_cast(u128, load_16(at - (past > 0 ? past : 0)));
   v = past >= N ? 0 : past > 0 ? v >> (past * 8 * (int)sizeof(T)) : v;
   return __builtin_bit_cast(uint4, v);
 }
@@ -109,16 +108,32 @@ struct Stage {
   static constexpr int kPer = ROWS * G / kThreads;
   static_assert(ROWS * G % kThreads == 0, "whole turns");
   uint4 r[kPer];
+  const T* at[kPer];
 
-  __device__ __forceinline__ void load(const T* p, int64_t ld, int row0, int rows, int k0,
-                                       int K, int tid) {
+  // The tiles are loaded one after the other from k0 on.
+  __device__ __forceinline__ void begin(const T* p, int64_t ld, int row0, int rows, int k0,
+                                        int tid) {
 #pragma unroll
     for (int i = 0; i < kPer; i++) {
       const int u = tid + i * kThreads;
-      const T* row = p + (int64_t)min(row0 + u / G, rows - 1) * ld;
-      const int k = k0 + u % G * GE;
-      r[i] = k0 + BK <= K ? __builtin_bit_cast(uint4, load_pack<T, GE>(row + k))
-                          : load_last<T, GE>(row, k, K);
+      at[i] = p + (int64_t)min(row0 + u / G, rows - 1) * ld + k0 + u % G * GE;
+    }
+  }
+  // A tile that does not hold the operand's last k.
+  __device__ __forceinline__ void load_next(int64_t) {
+#pragma unroll
+    for (int i = 0; i < kPer; i++) {
+      r[i] = load_16(at[i]);
+      at[i] += BK;
+    }
+  }
+  // Any tile; it begins at k0.
+  __device__ __forceinline__ void load_any(int64_t, int, int, int k0, int K, int tid) {
+#pragma unroll
+    for (int i = 0; i < kPer; i++) {
+      const int k = k0 + (tid + i * kThreads) % G * GE;
+      r[i] = load_end<T, GE>(at[i], k + GE - K, K);
+      at[i] += BK;
     }
   }
   __device__ __forceinline__ void store(uint4* lds, int tid) const {
@@ -156,21 +171,38 @@ struct Stage<T, false, ROWS, G> {
   static constexpr int kPer = BK * kWide / kThreads;
   static_assert(BK * kWide % kThreads == 0 && kThreads % kWide == 0, "whole turns");
   uint4 r[kPer];
+  const T* at[kPer];
 
   static __device__ __forceinline__ int turned(int k, int piece) {
     if (sizeof(T) == 4) return piece ^ ((k >> 2) & 1);
     return piece ^ (ROWS == 128 ? k & 3 : (k >> 1) & 1);
   }
-  __device__ __forceinline__ void load(const T* p, int64_t ld, int row0, int rows, int k0,
-                                       int K, int tid) {
+  __device__ __forceinline__ void begin(const T* p, int64_t ld, int row0, int rows, int k0,
+                                        int tid) {
 #pragma unroll
     for (int i = 0; i < kPer; i++) {
-      const int u = tid + i * kThreads, m = row0 + u % kWide * GE, k = k0 + u / kWide;
-      const T* row = p + (int64_t)k * ld;
-      if (k0 + BK <= K && row0 + ROWS <= rows)
-        r[i] = __builtin_bit_cast(uint4, load_pack<T, GE>(row + m));
-      else
-        r[i] = k < K ? load_last<T, GE>(row, m, rows) : make_uint4(0, 0, 0, 0);
+      const int u = tid + i * kThreads, m = row0 + u % kWide * GE;
+      at[i] = p + (int64_t)(k0 + u / kWide) * ld + (m < rows ? m : 0);
+    }
+  }
+  // A granule that the edge of the rows cuts is read whole: what lies past the
+  // edge is the row's padding or the next k row, which is there because the
+  // tile does not hold the last one.
+  __device__ __forceinline__ void load_next(int64_t ld) {
+#pragma unroll
+    for (int i = 0; i < kPer; i++) {
+      r[i] = load_16(at[i]);
+      at[i] += BK * ld;
+    }
+  }
+  __device__ __forceinline__ void load_any(int64_t ld, int row0, int rows, int k0, int K,
+                                           int tid) {
+#pragma unroll
+    for (int i = 0; i < kPer; i++) {
+      const int u = tid + i * kThreads, m = row0 + u % kWide * GE;
+      r[i] = make_uint4(0, 0, 0, 0);
+      if (k0 + u / kWide < K && m < rows) r[i] = load_end<T, GE>(at[i], m + GE - rows, rows);
+      at[i] += BK * ld;
     }
   }
   __device__ __forceinline__ void store(uint4* lds, int tid) const {
@@ -314,9 +346,13 @@ __global__ __launch_bounds__(kThreads, PER_CU) void k_product(ProductArgs a) {
   StageB sb;
   float sums[StageA::kSums] = {};
   const bool want_sums = !AKC && a.row_sums != nullptr && tn == 0;
-  auto load = [&](int k) {
-    sa.load((const T*)a.a, a.lda, m0, a.M, k * BK, a.K, tid);
-    sb.load((const T*)a.b, a.ldb, n0, a.N, k * BK, a.K, tid);
+  auto load_any = [&](int k) {
+    sa.load_any(a.lda, m0, a.M, k * BK, a.K, tid);
+    sb.load_any(a.ldb, n0, a.N, k * BK, a.K, tid);
+  };
+  auto load_next = [&]() {
+    sa.load_next(a.lda);
+    sb.load_next(a.ldb);
   };
   auto store = [&](int to) {
     sa.store(lds + to * kTile, tid);
@@ -330,19 +366,13 @@ __global__ __launch_bounds__(kThreads, PER_CU) void k_product(ProductArgs a) {
     for (int j = 0; j < TN; j++)
 #pragma unroll
       for (int e = 0; e < 16; e++) acc[i][j][e] = 0.0f;
-  load(first);
-  store(0);
-  __syncthreads();
-  int buffer = 0;
-  for (int k = first;;) {
-    if (k + 1 < last) load(k + 1);
+  auto multiply = [&](int buffer) {
     const uint4* from = lds + buffer * kTile;
 #pragma unroll
     for (int g = 0; g < G; g += 2) {
       uint4 fa[TM], fb[TN];
 #pragma unroll
-      for (int i = 0; i < TM; i++)
-        fa[i] = StageA::read(from, (wm * TM + i) * 32, g, lane);
+      for (int i = 0; i < TM; i++) fa[i] = StageA::read(from, (wm * TM + i) * 32, g, lane);
 #pragma unroll
       for (int j = 0; j < TN; j++)
         fb[j] = StageB::read(from + BM * G, (wn * TN + j) * 32, g, lane);
@@ -351,11 +381,36 @@ __global__ __launch_bounds__(kThreads, PER_CU) void k_product(ProductArgs a) {
 #pragma unroll
         for (int j = 0; j < TN; j++) acc[i][j] = Matrix<T>::mac32(fa[i], fb[j], acc[i][j]);
     }
-    if (++k >= last) break;
+  };
+  // Tiles before the last k are loaded without a test (rows of a few elements
+  // excepted, past whose end a granule would reach too far); a branch around
+  // the loads would wait for them at its end.
+  const int whole =
+      a.lda < StageA::GE || a.ldb < StageB::GE ? 0 : min(max((a.K - 1) / BK - first, 0), last - first);
+  sa.begin((const T*)a.a, a.lda, m0, a.M, first * BK, tid);
+  sb.begin((const T*)a.b, a.ldb, n0, a.N, first * BK, tid);
+  if (whole > 0)
+    load_next();
+  else
+    load_any(first);
+  store(0);
+  __syncthreads();
+  int buffer = 0, k = first + 1;
+  for (; k < first + whole; k++) {
+    load_next();
+    multiply(buffer);
     store(buffer ^ 1);
     __syncthreads();
     buffer ^= 1;
   }
+  for (; k < last; k++) {
+    load_any(k);
+    multiply(buffer);
+    store(buffer ^ 1);
+    __syncthreads();
+    buffer ^= 1;
+  }
+  multiply(buffer);
   __syncthreads();  // every wave has read its operands
 
   if (want_sums) {  // uniform over the block
