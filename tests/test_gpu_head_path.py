@@ -1,0 +1,81 @@
+"""The vocabulary head's operators together: the example of a small model
+taught by a large one, at a small size, and a training step with a draw
+captured in a graph."""
+import importlib.util
+import os
+
+import pytest
+
+from paper_1611_06172_amd import w2v
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def example():
+    spec = importlib.util.spec_from_file_location(
+        "smaller_vectors", os.path.join(ROOT, "examples", "smaller_vectors.py"))
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+def test_example_learns_and_draws():
+    import torch
+    losses, heads, drawn = example().main(V=2_000, topics=20, T=200_000, D=64, d=32, K=32,
+                                          epochs=2, steps=120, batch=512, rate=8.0,
+                                          verbose=False)
+    losses = losses.tolist()
+    print(f"[head path] loss {losses[0]:.4f} -> {losses[-1]:.4f}", flush=True)
+    assert all(v == v for v in losses)
+    # untaught, the student's loss is the teacher's distance from chance; a
+    # student that learns at all halves it
+    assert sum(losses[-10:]) < 0.5 * sum(losses[:10])
+    ids = drawn["ids"]
+    assert ids.shape == (4,) and (ids >= 0).all() and (ids < 2_000).all()
+    assert (drawn["logprob"] <= 0).all() and torch.isfinite(drawn["logprob"]).all()
+
+
+def test_step_and_draw_replayed_from_a_graph():
+    """Forward, distillation, backward and a draw, captured once and replayed
+    on new inputs, with eager work between the replays."""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+
+    def rand(*shape):
+        return torch.randn(shape, generator=g, device="cuda")
+
+    rows, V, D, K = 96, 150_001, 64, 20
+    x, w, b = rand(rows, D), rand(V, D) / 8, rand(V)
+    ids = torch.randint(0, V, (rows, K), generator=g, device="cuda", dtype=torch.int32)
+    teacher, u = rand(rows, K), torch.rand((rows, V), generator=g, device="cuda")
+    labels = torch.randint(0, V, (rows,), generator=g, device="cuda", dtype=torch.int32)
+
+    def step():
+        z = w2v.linear(x, w, b)
+        d = w2v.distill_loss(z, ids, teacher, temperature=2.0, labels=labels, soft=0.5,
+                             hard=0.5, want_grad=True)
+        back = w2v.linear_backward(d["grad"], x, w)
+        near = w2v.sample_words(z, u, top_k=30, top_p=0.9)
+        far = w2v.sample_words(z, u, top_p=0.9)
+        return [z, d["loss"], d["grad"], back["dx"], back["dw"], back["db"], near["ids"],
+                near["logprob"], far["ids"], far["logprob"]]
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for _ in range(4):
+        x.copy_(rand(rows, D))
+        u.copy_(torch.rand((rows, V), generator=g, device="cuda"))
+        eager = step()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(held, eager):
+            assert torch.equal(got, want)
