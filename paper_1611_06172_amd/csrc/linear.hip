@@ -6,13 +6,14 @@ namespace w2v {
 
 size_t linear_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t dtype) {
   if (M == 0 || few_rows(M, K)) return 0;
-  return partial_bytes(plan_product(M, N, K, dtype, false), M, N);
+  return partial_bytes(plan_product(M, N, K, dtype, false), M, N) +
+         copy_bytes(M, M, N, K, dtype) + copy_bytes(N, M, N, K, dtype);
 }
 
 size_t linear_backward_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t dtype,
                                        int32_t activation) {
   const BackwardPlan b = plan_backward(M, N, K, dtype, activation);
-  return b.dz + b.partial + b.sums;
+  return b.dz + b.partial + b.sums + b.x;
 }
 
 hipError_t launch_linear(const LinearArgs& a, void* workspace, hipStream_t s) {

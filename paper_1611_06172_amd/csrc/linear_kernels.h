@@ -572,6 +572,32 @@ __global__ __launch_bounds__(kThreads) void k_slope(const T* dy, int64_t lddy, c
   }
 }
 
+// Copies rows of K elements to rows of ldo, a wave a row.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_copy(const T* in, int64_t ld, T* out, int64_t ldo,
+                                                    int rows, int K) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= rows) return;
+  for (int col = (threadIdx.x & 63) * 8; col < K; col += 512) {
+    const uint4 v = load_end<T, 8>(in + row * ld + col, col + 8 - K, K);
+    __builtin_memcpy(out + row * ldo + col, &v, 16);
+  }
+}
+
+// An operand with rows on 64-byte lines: itself, or its copy at `copy`, which
+// has room for it unless it is not worth one (`bytes` 0).
+template <typename T>
+void align_rows(const void*& p, int64_t& ld, int rows, int K, void* copy, size_t bytes,
+                hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (bytes == 0 || ((uintptr_t)p % 64 == 0 && ld % 32 == 0)) return;
+    const int64_t ldo = aligned_columns(K);
+    k_copy<T><<<(int)ceil_div(rows, 4), kThreads, 0, s>>>((const T*)p, ld, (T*)copy, ldo, rows, K);
+    p = copy;
+    ld = ldo;
+  }
+}
+
 // Zeroes `bytes` bytes of each of `rows` rows, a wave a row.
 __global__ __launch_bounds__(kThreads) void k_zero(char* p, int64_t stride, int rows,
                                                     int64_t bytes) {
@@ -649,8 +675,13 @@ hipError_t launch_linear_as(const LinearArgs& l, void* workspace, hipStream_t s)
       k_few_rows<T, TO, 2><<<grid, kThreads, 0, s>>>(a);
     return hipGetLastError();
   }
-  return launch_product<T, TO, true, true>(a, plan_product(l.M, l.N, l.K, l.dtype, false), workspace,
-                                           nullptr, s);
+  const size_t bx = copy_bytes(l.M, l.M, l.N, l.K, l.dtype);
+  const size_t bw = copy_bytes(l.N, l.M, l.N, l.K, l.dtype);
+  char* ws = (char*)workspace;
+  align_rows<T>(a.a, a.lda, l.M, l.K, ws, bx, s);
+  align_rows<T>(a.b, a.ldb, l.N, l.K, ws + bx, bw, s);
+  return launch_product<T, TO, true, true>(a, plan_product(l.M, l.N, l.K, l.dtype, false),
+                                           ws + bx + bw, nullptr, s);
 }
 
 template <typename T>
@@ -670,6 +701,12 @@ hipError_t launch_backward_as(const LinearBackwardArgs& l, void* workspace, hipS
   ws += b.dz;
   void* partial = ws;
   float* sums = (float*)(ws + b.partial);
+  // (a copy of W for dx costs what it gains: its rows are read 256 bytes at a
+  // time)
+  const void* x = l.x;
+  int64_t ldx = l.ldx;
+  if (l.dw != nullptr || l.db != nullptr)
+    align_rows<T>(x, ldx, l.M, l.K, ws + b.partial + b.sums, b.x, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (l.M == 0) {  // no row: dW and db are sums of nothing
@@ -698,8 +735,8 @@ hipError_t launch_backward_as(const LinearBackwardArgs& l, void* workspace, hipS
     ProductArgs a{};
     a.a = dz;
     a.lda = lddz;
-    a.b = l.x;
-    a.ldb = l.ldx;
+    a.b = x;
+    a.ldb = ldx;
     a.M = l.N;
     a.N = l.K;
     a.K = l.M;

@@ -64,7 +64,10 @@ def test_linear_backward_rejects(over, needle):
 
 def test_linear_workspaces():
     import torch
-    assert w2v.linear_workspace_bytes(4_096, 71_290, 300, torch.bfloat16) == 0
+    assert w2v.linear_workspace_bytes(512, 1_000_000, 300, torch.float32) == 0
+    # copies of x and W with rows on 64-byte lines
+    assert w2v.linear_workspace_bytes(4_096, 71_290, 300, torch.bfloat16) >= \
+        (4_096 + 71_290) * 320 * 2
     assert w2v.linear_workspace_bytes(1, 1_000_000, 300, torch.float32) == 0
     n = w2v.linear_backward_workspace_bytes(64, 71_290, 300, torch.bfloat16)
     assert n > 0 and n % 256 == 0
