@@ -489,22 +489,25 @@ __global__ __launch_bounds__(THREADS) void k_row(Ctx c) {
   }
   if (STREAM) {
     constexpr int U = 4;
-    int64_t turn = head / (THREADS * N);
-    while (turn > 0) {
-      const int n = turn < U ? (int)turn : U;
-      turn -= n;
+    int64_t turn = head / kSpan;
+    for (; turn >= U; turn -= U) {
+      const T* from = in + (turn - U) * kSpan;
+      T* to = out + (turn - U) * kSpan;
       uint4 w[U];
 #pragma unroll
-      for (int u = 0; u < U; u++)
-        if (u < n) w[u] = load_16(in + ((turn + u) * THREADS + tid) * (int64_t)N);
+      for (int u = 0; u < U; u++) w[u] = load_16(from + u * kSpan + (uint32_t)(tid * N));
 #pragma unroll
       for (int u = 0; u < U; u++) {
-        if (u >= n) break;
         float v[N];
         unpack_words<T>(w[u], v);
-        store_pack<T, N>(out + ((turn + u) * THREADS + tid) * (int64_t)N,
-                         slopes<T, MODE>(g, v, c));
+        store_pack<T, N>(to + u * kSpan + (uint32_t)(tid * N), slopes<T, MODE>(g, v, c));
       }
+    }
+    for (; turn > 0; turn--) {
+      const int64_t at = (turn - 1) * kSpan + tid * N;
+      float v[N];
+      unpack_words<T>(load_16(in + at), v);
+      store_pack<T, N>(out + at, slopes<T, MODE>(g, v, c));
     }
   }
   __syncthreads();
