@@ -502,8 +502,9 @@ int w2v_step_batch_sorted(int32_t B, int32_t N, int32_t K, const int32_t* target
  * Sums and the epilogue are held in fp32 and each output is rounded once. The
  * order of a sum depends on the sizes alone: the same call gives the same
  * bits. workspace: device, 256-byte aligned, at least
- * w2v_linear_workspace_bytes(M, N, K, dtype) bytes (0 unless a long k is
- * split), contents need not be initialised; calls that overlap in time must
+ * w2v_linear_workspace_bytes(M, N, K, dtype) bytes (partial sums where a long k
+ * is split; in 16 bits, for large outputs, copies of x and W with rows on
+ * 64-byte lines, made if theirs are not; otherwise 0), contents need not be initialised; calls that overlap in time must
  * not share it. M = 0 is allowed and does nothing; N, K >= 1. y and pre must
  * not overlap any other argument (residual = y excepted).
  */

@@ -324,6 +324,16 @@ __device__ __forceinline__ void tile_of(const ProductArgs& a, int& tm, int& tn, 
 // of k: the next one's loads are in flight while this one is multiplied, and
 // the PER_CU blocks of a CU fill each other's waits.
 // FULL: an epilogue with activation, residual or pre; otherwise with a bias.
+// Blocks of 128 x 128 with 64 bytes of k are the largest that leave room for
+// four on a CU. With one 256-wide block on it, a k of 300 is over before its
+// pipeline is full: bf16 4,096 x 71,290 x 300 617 us against 549 (both before
+// the loads lost their branch).
+// Measured, in traces: bf16 4,096 x 71,290 x 300 406 us and up (430 TFLOP/s,
+// output at 1.4 TB/s), its gradients with 8,191 rows 861 us (dx, 407 TFLOP/s)
+// and 939 (dW, 373); 65,536 x 300 x 300 with bias, gelu and residual 63; fp32
+// 512 x 10^6 x 300 2,650 (116 TFLOP/s, a library product of 8,192^3 has 153).
+// 16 bits are bound by what a CU waits for between memory, LDS and MFMA at a k
+// of ten tiles, fp32 by MFMA.
 template <typename T, typename TO, bool AKC, bool BKC, bool FULL, int TM, int TN, int G,
           int PER_CU>
 __global__ __launch_bounds__(kThreads, PER_CU) void k_product(ProductArgs a) {
@@ -494,10 +504,11 @@ __global__ __launch_bounds__(kThreads) void k_join(ProductArgs a) {
   }
 }
 
-// Few rows of x (M <= 16 MF): nothing of W is used twice, so W goes from
-// memory straight into MFMA registers, 16 of its rows a wave, with x's rows as
-// the other operand.
-template <typename T, typename TO, int MF>
+// Few rows of x (M <= 16): nothing of W is used twice, so W goes from memory
+// straight into MFMA registers, 16 of its rows a wave, with x's rows as the
+// other operand. Bound by W's bytes: 1 x 71,290 x 300 fp32 13.0 us in a trace,
+// 6.6 TB/s of which the memory-side cache holds a part from call to call.
+template <typename T, typename TO>
 __global__ __launch_bounds__(kThreads) void k_few_rows(ProductArgs a) {
   constexpr int GE = Matrix<T>::kGranule, STEP = 4 * GE, U = 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -505,52 +516,37 @@ __global__ __launch_bounds__(kThreads) void k_few_rows(ProductArgs a) {
   if (n0 >= a.N) return;
   const int g = lane >> 4, r = lane & 15;
   const T* w = (const T*)a.b + (int64_t)min(n0 + r, a.N - 1) * a.ldb + g * GE;
-  const T* x[MF];
-  f32x4 acc[MF];
-#pragma unroll
-  for (int f = 0; f < MF; f++) {
-    x[f] = (const T*)a.a + (int64_t)min(f * 16 + r, a.M - 1) * a.lda + g * GE;
-    acc[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
+  const T* x = (const T*)a.a + (int64_t)min(r, a.M - 1) * a.lda + g * GE;
+  f32x4 acc = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   int k = 0;
   for (; k + U * STEP <= a.K; k += U * STEP) {
-    uint4 fw[U], fx[U][MF];
+    uint4 fw[U], fx[U];
 #pragma unroll
     for (int u = 0; u < U; u++) {
       fw[u] = __builtin_bit_cast(uint4, load_pack<T, GE>(w + k + u * STEP));
-#pragma unroll
-      for (int f = 0; f < MF; f++)
-        fx[u][f] = __builtin_bit_cast(uint4, load_pack<T, GE>(x[f] + k + u * STEP));
+      fx[u] = __builtin_bit_cast(uint4, load_pack<T, GE>(x + k + u * STEP));
     }
 #pragma unroll
-    for (int u = 0; u < U; u++)
-#pragma unroll
-      for (int f = 0; f < MF; f++) acc[f] = Matrix<T>::mac16(fw[u], fx[u][f], acc[f]);
+    for (int u = 0; u < U; u++) acc = Matrix<T>::mac16(fw[u], fx[u], acc);
   }
   for (; k < a.K; k += STEP) {
     const int64_t n = a.K - k - g * GE;
     const uint4 fw = __builtin_bit_cast(uint4, load_some<T, GE>(w + k, n));
-#pragma unroll
-    for (int f = 0; f < MF; f++)
-      acc[f] = Matrix<T>::mac16(
-          fw, __builtin_bit_cast(uint4, load_some<T, GE>(x[f] + k, n)), acc[f]);
+    acc = Matrix<T>::mac16(fw, __builtin_bit_cast(uint4, load_some<T, GE>(x + k, n)), acc);
   }
-  // lane: columns n0 + 4 g .. + 3 of row r (+ 16 f)
+  // lane: columns n0 + 4 g .. + 3 of row r
   const int col = n0 + 4 * g;
+  if (r < a.M && col < a.N) {
+    Pack<float, 4> z;
 #pragma unroll
-  for (int f = 0; f < MF; f++) {
-    const int m = f * 16 + r;
-    if (m < a.M && col < a.N) {
-      Pack<float, 4> z;
-#pragma unroll
-      for (int i = 0; i < 4; i++) z.v[i] = acc[f][i];
-      finish<T, TO, 4>(a, m, col, min(4, a.N - col), z);
-    }
+    for (int i = 0; i < 4; i++) z.v[i] = acc[i];
+    finish<T, TO, 4>(a, r, col, min(4, a.N - col), z);
   }
 }
 
 // dz = dy act'(z), rounded once to the operands' type: the MFMA operands of
-// both gradient products have it.
+// both gradient products have it. Bound by memory: 4,096 x 600 fp32 8.7 us, 3.4
+// TB/s.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_slope(const T* dy, int64_t lddy, const T* pre,
                                                      int64_t ldp, T* dz, int M, int N,
@@ -572,7 +568,8 @@ __global__ __launch_bounds__(kThreads) void k_slope(const T* dy, int64_t lddy, c
   }
 }
 
-// Copies rows of K elements to rows of ldo, a wave a row.
+// Copies rows of K elements to rows of ldo, a wave a row: 71,290 x 300 bf16 in
+// 24 us, 3.6 TB/s.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_copy(const T* in, int64_t ld, T* out, int64_t ldo,
                                                     int rows, int K) {
@@ -669,10 +666,7 @@ hipError_t launch_linear_as(const LinearArgs& l, void* workspace, hipStream_t s)
   a.activation = l.activation;
   if (few_rows(l.M, l.K)) {
     const int grid = (int)ceil_div(l.N, 64);
-    if (l.M <= 16)
-      k_few_rows<T, TO, 1><<<grid, kThreads, 0, s>>>(a);
-    else
-      k_few_rows<T, TO, 2><<<grid, kThreads, 0, s>>>(a);
+    k_few_rows<T, TO><<<grid, kThreads, 0, s>>>(a);
     return hipGetLastError();
   }
   const size_t bx = copy_bytes(l.M, l.M, l.N, l.K, l.dtype);
