@@ -4,9 +4,10 @@
 //   p_1 = softmax(s),
 //   loss = soft T^2 sum_k q_k (log q_k - log p_T(id_k)) - hard log p_1(label)
 //   d loss / d s_j = soft T (Q p_T(j) - q_j) + hard (p_1(j) - [j = label])
-// with Q = 1 where the row lists a word, else 0. One pass over s keeps a
-// running maximum and the two sums of exponentials relative to it; a second
-// one forms the gradient. Both are bound by memory.
+// with Q = 1 where the row lists a word, else 0. A block that can hold a row in
+// its registers reads it once (k_row); otherwise one pass over s keeps a running
+// maximum and the two sums of exponentials relative to it, and a second one
+// forms the gradient. All are bound by memory.
 #include "distill.h"
 
 #include "head_types.h"
@@ -397,7 +398,12 @@ __device__ __forceinline__ uint4 load_few(const T* row, int64_t at, int64_t V) {
 // Loss and gradient of a row by one block. The end of the row stays in
 // registers, NV packs of 16 bytes a thread, between the sums and the gradient;
 // STREAM: of longer rows the first part is read twice, the second time
-// backwards, from what was read last.
+// backwards, from what was read last. Measured (us, bf16, K 64): 4,096 rows of
+// 71,290 261 to 290, 4.0 to 4.5 TB/s, where a copy of them has 4.9; 65,536 of
+// 1,000 87; 2,048 of 10^6 2,390, whose two readings and one writing pass at
+// 4.9 TB/s of traffic.
+// Between its sums and its gradient a block waits for its slowest wave; two
+// blocks a CU (18 packs are 72 of 128 registers) fill each other's waits.
 template <typename T, int MODE, int THREADS, int NV, bool STREAM>
 __global__ __launch_bounds__(THREADS) void k_row(Ctx c) {
   const List l = list_of(c);
@@ -537,6 +543,16 @@ Ctx context(const DistillArgs& a) {
   return c;
 }
 
+// A row goes to the smallest block whose registers hold it: of 65,536 rows of
+// 1,000 bf16 one of 64 threads takes 87 us, of 256 253; 16,384 rows of 8,000 256
+// threads 138, 512 291; 4,096 of 30,000 9 packs a thread 134, 18 165; 4,096 of
+// 71,290 512 threads 261, 1,024 425. (K <= 128: a wave alone does not go through
+// longer lists.) By shares (k_sums, k_loss, k_gradient) these take 399 (the
+// last), and with few rows no less either: 8 rows of 71,290 24 beside 22, 16 of
+// 1,000 28 beside 17.
+// Longer rows, which a block reads twice in part, need enough rows to fill the
+// GPU. By a block and by shares: 2,048 rows of 110,000 295 and 317, 64 30 and
+// 29, one 28 and 25; 256 rows of 10^6 300 and 329, 128 194 and 166, 16 133 and 42.
 template <typename T, int MODE>
 hipError_t launch_as(const Ctx& c, bool forward, hipStream_t s) {
   constexpr int N = 16 / (int)sizeof(T);
@@ -550,7 +566,7 @@ hipError_t launch_as(const Ctx& c, bool forward, hipStream_t s) {
     k_row<T, MODE, 512, 9, false><<<rows, 512, lds, s>>>(c);
   } else if (forward && V <= 512 * 18 * N) {
     k_row<T, MODE, 512, 18, false><<<rows, 512, lds, s>>>(c);
-  } else if (forward && (V <= 1024 * 14 * N || rows >= kCUs)) {
+  } else if (forward && rows >= kCUs) {
     k_row<T, MODE, 1024, 14, true><<<rows, 1024, lds, s>>>(c);
   } else {
     const int grid = rows * c.splits;
