@@ -329,8 +329,8 @@ __device__ __forceinline__ void tile_of(const ProductArgs& a, int& tm, int& tn, 
 // pipeline is full: bf16 4,096 x 71,290 x 300 617 us against 549 (both before
 // the loads lost their branch).
 // Measured, in traces: bf16 4,096 x 71,290 x 300 406 us and up (430 TFLOP/s,
-// output at 1.4 TB/s), its gradients with 8,191 rows 861 us (dx, 407 TFLOP/s)
-// and 939 (dW, 373); 65,536 x 300 x 300 with bias, gelu and residual 63; fp32
+// output at 1.4 TB/s), its gradients with 8,191 rows 939 us (dx, 373 TFLOP/s)
+// and 861 (dW, 407); 65,536 x 300 x 300 with bias, gelu and residual 63; fp32
 // 512 x 10^6 x 300 2,650 (116 TFLOP/s, a library product of 8,192^3 has 153).
 // 16 bits are bound by what a CU waits for between memory, LDS and MFMA at a k
 // of ten tiles, fp32 by MFMA.

@@ -2,6 +2,8 @@
 // workspace (host only).
 #pragma once
 
+#include <cmath>
+
 #include "linear.h"
 #include "w2v.h"
 
@@ -26,18 +28,30 @@ struct Plan {
 // Blocks that the GPU holds at once, 4 on each of 256 CUs.
 constexpr int kSlots = 1024;
 
-// The tile whose padded output costs least. What a tile's element costs beside
-// one of a 128 x 128 tile, by products that fill the GPU (8192 x 8192 outputs,
-// k 2048): fp32, bound by MFMA, 1.10 for 64 x 64 and 1.07 for 128 x 64; 16 bits,
-// bound by LDS reads, 1.8 and 1.45, but 1.35 and 1.15 where both operands are
-// turned (dW). An output with fewer tiles than the GPU holds blocks leaves
-// that share of it idle: bf16 65,536 x 300 x 300 takes 42 us with 128 x 128
-// tiles and 51 with 64 x 64 ones, 4,096 x 600 x 600 29 and 17.
-// A product with a long k and few tiles is split along k into as many blocks
-// as the GPU holds, of at least 8 tiles of k each.
+// Share of the GPU's rate that so many blocks reach: one block a CU is half of
+// it, four are all. (fp32 4,096 x 600 x 600 with 160, 320 and 640 blocks took
+// 65, 54 and 43 us.)
+inline double filled(double blocks) {
+  if (blocks >= kSlots) return 1.0;
+  const double cus = kSlots / 4.0;
+  return blocks >= cus ? std::sqrt(blocks / kSlots) : 0.5 * blocks / cus;
+}
+
+// The tile and the split of k with the least time. What a tile's element costs
+// beside one of a 128 x 128 tile, by products that fill the GPU (8192 x 8192
+// outputs, k 2048): fp32, bound by MFMA, 1.10 for 64 x 64 and 1.07 for 128 x 64;
+// 16 bits, bound by LDS reads, 1.8 and 1.45, but 1.35 and 1.15 where both
+// operands are turned (dW). bf16 65,536 x 300 x 300 takes 42 us with 128 x 128
+// tiles and 51 with 64 x 64 ones.
+// A k may be split into as many parts as the GPU has room for, of at least 8
+// tiles of k each. Partial sums are written and read at 4 TB/s, and one more
+// launch takes 3 us: bf16 4,096 x 600 x 600 takes 26 us in two parts, 14.5 in
+// one, fp32 4,096 x 300 x 300 23 and 18; but dW of 4,096 x 600 x 600 fp32 (600 x
+// 600 outputs) takes 116 in one, 46 in ten.
 inline Plan plan_product(int32_t M, int32_t N, int32_t K, int32_t dtype, bool both_turned) {
   static const double kCost[3][3] = {{1.10, 1.07, 1.0}, {1.8, 1.45, 1.0}, {1.35, 1.15, 1.0}};
   const double* cost = kCost[dtype == W2V_DTYPE_F32 ? 0 : both_turned ? 2 : 1];
+  const double rate = dtype == W2V_DTYPE_F32 ? 115e6 : 420e6;  // operations a us
   Plan best{};
   double least = 0.0;
   for (int i = 2; i >= 0; i--) {
@@ -48,18 +62,20 @@ inline Plan plan_product(int32_t M, int32_t N, int32_t K, int32_t dtype, bool bo
     p.tiles_n = (int32_t)ceil_div(N, t.cols);
     const int64_t k_tiles = ceil_div(K, t.granules * 16 / element_size(dtype));
     const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
-    int64_t splits = kSlots / tiles;
-    if (splits > k_tiles / 8) splits = k_tiles / 8;
-    if (splits > 64) splits = 64;
-    if (splits < 1) splits = 1;
-    p.k_per_split = (int32_t)ceil_div(k_tiles, splits);
-    p.splits = (int32_t)ceil_div(k_tiles, p.k_per_split);
-    const double blocks = (double)tiles * p.splits;
-    double c = cost[i] * (double)tiles * t.rows * t.cols;
-    if (blocks < kSlots) c *= kSlots / blocks;
-    if (i == 2 || c < least) {
-      best = p;
-      least = c;
+    int64_t most = kSlots / tiles;
+    if (most > k_tiles / 8) most = k_tiles / 8;
+    if (most > 64) most = 64;
+    if (most < 1) most = 1;
+    const double work = cost[i] * (double)tiles * t.rows * t.cols * 2.0 * K / rate;
+    for (int64_t splits = 1; splits <= most; splits++) {
+      p.k_per_split = (int32_t)ceil_div(k_tiles, splits);
+      p.splits = (int32_t)ceil_div(k_tiles, p.k_per_split);
+      double us = work / filled((double)tiles * p.splits);
+      if (p.splits > 1) us += 3.0 + 2.0 * p.splits * (double)M * N * 4.0 / 4e6;
+      if ((i == 2 && splits == 1) || us < least) {
+        best = p;
+        least = us;
+      }
     }
   }
   return best;
