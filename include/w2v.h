@@ -522,7 +522,8 @@ int w2v_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, const flo
  * the residual's gradient is dy itself. dx, dw and db may each be NULL (not
  * wanted). pre: z as w2v_linear wrote it, needed unless the activation is
  * W2V_ACTIVATION_NONE; relu's derivative at 0 is 0. All matrices are of
- * `dtype`. With an activation, dz is rounded once to `dtype`; sums are held in
+ * `dtype`. With an activation, dz is rounded once to `dtype` for dx and dW; db
+ * sums it before that rounding. Sums are held in
  * fp32, in an order that depends on the sizes alone. M = 0 gives dW = 0 and
  * db = 0. workspace: as above, w2v_linear_backward_workspace_bytes bytes.
  * Outputs must not overlap any other argument.

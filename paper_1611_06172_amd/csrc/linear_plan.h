@@ -108,9 +108,31 @@ inline size_t copy_bytes(int32_t rows, int32_t M, int32_t N, int32_t K, int32_t 
 // 55 and 34; 32 x 71,290 x 300 bf16 with two operands 17.9 and 14.9.
 inline bool few_rows(int32_t M, int32_t K) { return M <= 16 && K <= 2048; }
 
+// Blocks of k_slope_sums: stripes of up to 32 packs of 16 bytes, as even as they
+// come, by chunks of rows, about 2048 blocks in all and at most 1024 chunks, whose
+// sums are added up afterwards.
+struct SlopePlan {
+  int32_t stripes, chunks, across, rows;
+};
+
+inline SlopePlan plan_slope(int32_t M, int32_t N, int32_t dtype) {
+  SlopePlan p;
+  const int64_t packs = ceil_div(N, 16 / element_size(dtype));
+  p.stripes = (int32_t)ceil_div(packs, 32);
+  p.across = (int32_t)ceil_div(packs, p.stripes);
+  const int64_t down = 256 / p.across;  // rows that a block has at once
+  int64_t chunks = ceil_div(2048, p.stripes);
+  if (chunks > 1024) chunks = 1024;
+  p.rows = (int32_t)(ceil_div(ceil_div(M, chunks), down) * down);
+  p.chunks = (int32_t)ceil_div(M, p.rows);
+  return p;
+}
+
 // The backward pass's parts of its workspace.
 struct BackwardPlan {
   Plan dx, dw;
+  bool apart;  // db is summed beside dz; otherwise within dW's product
+  SlopePlan slope;  // where it is
   size_t dz, partial, sums, x;  // bytes
 };
 
@@ -123,9 +145,12 @@ inline BackwardPlan plan_backward(int32_t M, int32_t N, int32_t K, int32_t dtype
   b.dz = activation == W2V_ACTIVATION_NONE
              ? 0
              : aligned((size_t)M * N * element_size(dtype));
+  b.apart = b.dz != 0 && dtype != W2V_DTYPE_F32;  // dz is rounded to 16 bits
+  if (b.apart) b.slope = plan_slope(M, N, dtype);
   const size_t px = partial_bytes(b.dx, M, K), pw = partial_bytes(b.dw, N, K);
   b.partial = px > pw ? px : pw;
-  b.sums = b.dw.splits == 1 ? 0 : aligned((size_t)b.dw.splits * N * 4);
+  const int32_t parts = b.apart ? b.slope.chunks : b.dw.splits;
+  b.sums = parts == 1 ? 0 : aligned((size_t)parts * N * 4);
   b.x = copy_bytes(M, M, N, K, dtype);
   return b;
 }

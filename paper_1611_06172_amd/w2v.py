@@ -668,7 +668,8 @@ def linear_backward(dy, x, weight, *, activation: str = "none", pre=None,
     """Gradients of linear() from dy (M, N): a dict of dx (M, K) and dw (N, K)
     in x's type and db float32 (N,), None where not wanted
     (w2v_linear_backward). pre: what linear() wrote, needed with an
-    activation. The residual's gradient is dy."""
+    activation; dy act'(pre) is then rounded to x's type for dx and dw, and
+    summed before that for db. The residual's gradient is dy."""
     import torch
     code = _head_dtype(x, "x")
     ldx = _operand(x, "x")

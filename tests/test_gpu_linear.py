@@ -178,6 +178,32 @@ def test_backward(M, N, K, activation, name):
           eps * dz.abs().sum(dim=0) + low * M)
 
 
+@pytest.mark.parametrize("name", ["bfloat16", "float16"])
+@pytest.mark.parametrize("activation", ["relu", "gelu", "silu", "tanh", "sigmoid"])
+@pytest.mark.parametrize("M,N,K", [(1, 70, 33), (2, 9_001, 8), (67, 129, 65), (300, 1031, 31),
+                                   (4_099, 600, 24), (20_003, 41, 9)])
+def test_bias_gradient_is_summed_before_dz_is_rounded(M, N, K, activation, name):
+    """db is float32 and holds dz = dy act'(pre) of 32 bits: a slope is within
+    8 units of 2^-24 of 1.13, the product adds one, and no term goes through
+    more than 160 additions (rows of a thread, threads of a block, blocks).
+    dz rounded to the operands' type first would be 2^-9 or 2^-12 off."""
+    import torch
+    g = generator(M + 2 * N + 3 * K)
+    x, w = matrix(g, M, K, name, pad=1), matrix(g, N, K, name, N ** -0.5, pad=2)
+    dy, pre = matrix(g, M, N, name, pad=3), matrix(g, M, N, name, 2.0, pad=1)
+    out = w2v.linear_backward(dy, x, w, activation=activation, pre=pre)
+    dy64 = dy.double().cpu()
+    exact = (dy64 * slope64(pre.double().cpu(), activation)).sum(dim=0)
+    bound = (9 + min(M, 160)) * 2.0 ** -24 * 1.13 * dy64.abs().sum(dim=0) + 1e-30
+    worst = ((out["db"].double().cpu() - exact).abs() / bound).max().item()
+    assert worst <= 1.0, worst
+    # alone, and beside dx without dW: the same sums
+    for kw in (dict(want_dx=False, want_dw=False), dict(want_dw=False)):
+        part = w2v.linear_backward(dy, x, w, activation=activation, pre=pre, **kw)
+        assert torch.equal(part["db"], out["db"]) and part["dw"] is None
+    rest = w2v.linear_backward(dy, x, w, activation=activation, pre=pre, want_db=False)
+    assert torch.equal(rest["dx"], out["dx"]) and torch.equal(rest["dw"], out["dw"])
+
 @pytest.mark.parametrize("name", ["float32", "bfloat16"])
 def test_backward_splits_long_sums(name):
     """dx sums over many words, dW and db over many rows: both split."""
