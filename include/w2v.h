@@ -547,7 +547,7 @@ int w2v_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx
  *              not looked at); a row may have none (no soft term). Entries of
  *              one word add up;
  *   teacher    device [rows][K] of teacher_dtype: the teacher's logits; -inf
- *              gives q = 0;
+ *              gives q = 0, and a row of such entries alone has no soft term;
  *   labels     device int32[rows] or NULL (no hard term); -1 = none;
  *   row_weight device float[rows] or NULL (1): scales the row's gradient, not
  *              its loss;
@@ -557,8 +557,8 @@ int w2v_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx
  *              what w2v_distill_backward needs;
  *   grad       device rows x V of `dtype`, stride ldg, or NULL (not wanted):
  *              row_weight (soft T (Q p_T - q) + hard (p_1 - [label])), Q = 1 if
- *              the row has an entry, else 0. May be the logits' own memory
- *              (same stride), not overlap them otherwise.
+ *              the row has an entry above -inf, else 0. May be the logits' own
+ *              memory (same stride), not overlap them otherwise.
  * A row whose scores are all -inf has loss 0 and gradient 0. NaN or +inf
  * among a row's scores or present teacher logits makes its loss NaN. A row
  * with an id or a label outside [-1, V) has loss 0 and gradient 0 and is

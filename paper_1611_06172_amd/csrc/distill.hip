@@ -4,10 +4,10 @@
 //   p_1 = softmax(s),
 //   loss = soft T^2 sum_k q_k (log q_k - log p_T(id_k)) - hard log p_1(label)
 //   d loss / d s_j = soft T (Q p_T(j) - q_j) + hard (p_1(j) - [j = label])
-// with Q = 1 where the row lists a word, else 0. A block that can hold a row in
-// its registers reads it once (k_row); otherwise one pass over s keeps a running
-// maximum and the two sums of exponentials relative to it, and a second one
-// forms the gradient. All are bound by memory.
+// with Q = 1 where the row lists a word above -inf, else 0. A block that can
+// hold a row in its registers reads it once (k_row); otherwise one pass over s
+// keeps a running maximum and the two sums of exponentials relative to it, and a
+// second one forms the gradient. All are bound by memory.
 #include "distill.h"
 
 #include "head_types.h"
@@ -143,7 +143,7 @@ __device__ __forceinline__ List list_of(const Ctx& c) {
 }
 
 struct Row {
-  bool some;       // lists a word
+  bool some;       // lists a word whose logit is above -inf
   bool ok;         // every id is a word or -1
   int32_t label;   // or -1
   float weight;    // of the gradient
@@ -300,8 +300,10 @@ __device__ __forceinline__ Slope begin_gradient(const Ctx& c, const Row& r, cons
   const float soft = r.weight * c.a.soft * c.a.temperature, hard = r.weight * c.a.hard;
   const bool live = r.ok && log_soft != -INFINITY;
   for (int k = threadIdx.x; k <= c.a.K; k += blockDim.x) {
-    l.q[k] = k == c.a.K ? hard : l.id[k] < 0 ? 0.0f : soft * expf(log_q(c, r, l.q[k]));
-    if (!live || l.id[k] < lo || l.id[k] >= hi) l.id[k] = -1;
+    // (where every present logit is -inf there is no q to form)
+    const bool there = live && l.id[k] >= lo && l.id[k] < hi && (k == c.a.K || r.some);
+    if (!there) l.id[k] = -1;
+    l.q[k] = k == c.a.K ? hard : there ? soft * expf(log_q(c, r, l.q[k])) : 0.0f;
   }
   __syncthreads();
   Slope g = {max, 0.0f, 0.0f, true};

@@ -239,6 +239,43 @@ def test_nan_and_infinity_show_in_their_row():
         assert out["loss"][6] == float("inf") and torch.isfinite(out["loss"][7])
 
 
+@pytest.mark.parametrize("name", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("V", [5, 500, 30_000, 100_000, 200_001])
+def test_list_of_masked_words_alone_is_no_list(V, name):
+    """A row whose present teacher logits are all -inf has nothing to learn
+    from: no soft term in its loss or its gradient, like a row of absent
+    entries; one entry above -inf is a list of that entry."""
+    import torch
+    c = case(6, V, 4, name, V, masked=False)
+    ids = c["ids"]
+    ids[:] = torch.randint(0, V, ids.shape)
+    c["teacher"].fill_(float("-inf"))
+    c["teacher"][4, 2] = 1.0
+    ids[5, 3] = -1
+    c["labels"][0] = ids[0, 1]
+    c["labels"][5] = 3
+    absent = dict(c, ids=ids.clone())
+    absent["ids"][[0, 1, 2, 3, 5]] = -1
+    for labels in (True, False):
+        kw = dict(temperature=2.0, soft=0.7, hard=0.3)
+        one = dict(absent, labels=c["labels"] if labels else None)
+        kw["labels"] = one["labels"]
+        loss, lb, grad, gb = exact(
+            dict(one, ids=torch.where(one["teacher"] > -1, one["ids"],
+                                      torch.full_like(one["ids"], -1))), 2.0, 0.7, 0.3)
+        want = w2v.distill_loss(one["logits"], one["ids"], one["teacher"], want_grad=True, **kw)
+        got = w2v.distill_loss(c["logits"], ids, c["teacher"], want_grad=True, **kw)
+        assert torch.isfinite(got["loss"]).all() and torch.isfinite(got["grad"]).all()
+        assert ((got["loss"].double().cpu() - loss).abs() <= lb + U * loss.abs()).all()
+        assert torch.equal(got["loss"], want["loss"])
+        assert torch.equal(got["grad"], want["grad"])
+        back = w2v.distill_backward(torch.ones(6, device="cuda"), c["logits"], ids,
+                                    c["teacher"], got["stats"], **kw)
+        there = w2v.distill_backward(torch.ones(6, device="cuda"), one["logits"], one["ids"],
+                                     one["teacher"], want["stats"], **kw)
+        assert torch.isfinite(back).all() and torch.equal(back, there)
+
+
 @pytest.mark.parametrize("V", [100, 30_000, 90_000])
 def test_ids_outside_the_vocabulary_skip_the_row(V):
     import torch
