@@ -560,9 +560,10 @@ int w2v_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx
  *              the row has an entry above -inf, else 0. May be the logits' own
  *              memory (same stride), not overlap them otherwise.
  * A row whose scores are all -inf has loss 0 and gradient 0. NaN or +inf
- * among a row's scores or present teacher logits makes its loss NaN. A row
- * with an id or a label outside [-1, V) has loss 0 and gradient 0 and is
- * recorded in the device's error word. Sums, statistics and loss are held in
+ * among a row's scores makes its loss and its whole gradient NaN, whatever
+ * terms the row has; among its present teacher logits, its loss. A row with an
+ * id or a label outside [-1, V) has loss 0 and gradient 0 and is recorded in
+ * the device's error word. Sums, statistics and loss are held in
  * fp32; the gradient is rounded once. The same call gives the same bits.
  * Limits: 0 <= K <= W2V_MAX_TEACHER, temperature in [2^-20, 2^20], rows >= 0,
  * V >= 1. workspace: device, 256-byte aligned, at least

@@ -220,10 +220,16 @@ __global__ __launch_bounds__(kThreads) void k_sums(Ctx c) {
   }
 }
 
+// log of a row's second sum, which is 0 where nothing was added to it. NaN, as a
+// score of NaN or +inf makes it, stays.
+__device__ __forceinline__ float log_hard_of(const Sums& s) {
+  return s.hard == 0.0f ? 0.0f : logf(s.hard);
+}
+
 // A row's loss from its sums (every thread has them); thread 0 writes it.
 __device__ __forceinline__ void write_loss(const Ctx& c, int row, const Row& r, const List& l,
                                            const Sums& s) {
-  const float log_soft = logf(s.soft), log_hard = s.hard > 0.0f ? logf(s.hard) : 0.0f;
+  const float log_soft = logf(s.soft), log_hard = log_hard_of(s);
   const bool live = r.ok && log_soft != -INFINITY;  // some score is above -inf
   float v = 0.0f;
   if (live && r.some) {
@@ -238,6 +244,7 @@ __device__ __forceinline__ void write_loss(const Ctx& c, int row, const Row& r, 
   if (threadIdx.x == 0) {
     float loss = c.a.soft * c.a.temperature * c.a.temperature * v;
     if (live && r.label >= 0) loss += c.a.hard * (log_hard - (l.s[c.a.K] - s.max));
+    if (log_soft != log_soft) loss = NAN;  // whatever terms the row has
     if (!live) loss = 0.0f;
     c.a.loss[row] = loss;
     c.a.stats[(int64_t)row * 3] = s.max;
@@ -307,7 +314,7 @@ __device__ __forceinline__ Slope begin_gradient(const Ctx& c, const Row& r, cons
   }
   __syncthreads();
   Slope g = {max, 0.0f, 0.0f, true};
-  if (live && r.some) {
+  if (live && (r.some || log_soft != log_soft)) {  // NaN reaches every row's gradient
     g.soft = soft * expf(-log_soft);
     g.none = false;
   }
@@ -477,7 +484,7 @@ __global__ __launch_bounds__(THREADS) void k_row(Ctx c) {
   write_loss(c, (int)row, r, l, s);
   if (c.a.grad == nullptr) return;
 
-  const float log_soft = logf(s.soft), log_hard = s.hard > 0.0f ? logf(s.hard) : 0.0f;
+  const float log_soft = logf(s.soft), log_hard = log_hard_of(s);
   const Slope g = begin_gradient(c, r, l, s.max, log_soft, log_hard, 0, V);
   T* out = (T*)c.a.grad + row * c.a.ldg;
 #pragma unroll

@@ -276,6 +276,40 @@ def test_list_of_masked_words_alone_is_no_list(V, name):
         assert torch.isfinite(back).all() and torch.equal(back, there)
 
 
+@pytest.mark.parametrize("rows,V", [(12, 7), (12, 600), (12, 20_000), (12, 60_000),
+                                    (12, 100_000), (260, 40_001)])
+@pytest.mark.parametrize("T", [1.0, 2.0, 3.0])
+def test_nan_and_infinity_show_without_a_list(rows, V, T):
+    """A score of NaN or +inf makes its row's loss and gradient NaN whatever
+    terms the row has: a label alone, a list alone, both or neither."""
+    import torch
+    c = case(rows, V, 5, "float32", V, masked=False)
+    c["teacher"] = torch.nan_to_num(c["teacher"], nan=0.0)
+    c["ids"].clamp_(min=0)
+    c["ids"][:8] = -1  # rows 0 to 7: no list
+    c["labels"][:] = 1
+    c["labels"][4:10] = -1  # rows 4 to 9: no label
+    z = c["logits"]
+    z[3] = 0.25
+    bad = [0, 1, 4, 5, 8, 10]
+    for r in bad:
+        z[r, V - 1 if r % 2 else 3] = float("inf" if r in (1, 5, 10) else "nan")
+    good = [r for r in range(rows) if r not in bad]
+    clean = z.clone()
+    clean[bad] = 0.0
+    one = torch.ones(rows, device="cuda")
+    for ids, teacher in ((c["ids"], c["teacher"]),
+                         (c["ids"][:, :0].contiguous(), c["teacher"][:, :0].contiguous())):
+        kw = dict(temperature=T, labels=c["labels"], hard=0.5)
+        out = w2v.distill_loss(z, ids, teacher, want_grad=True, **kw)
+        want = w2v.distill_loss(clean, ids, teacher, want_grad=True, **kw)
+        back = w2v.distill_backward(one, z, ids, teacher, out["stats"], **kw)
+        assert torch.isnan(out["loss"][bad]).all()
+        assert torch.isnan(out["grad"][bad]).all() and torch.isnan(back[bad]).all()
+        for key in ("loss", "grad"):
+            assert torch.equal(out[key][good], want[key][good])
+        assert torch.isfinite(back[good]).all()
+
 @pytest.mark.parametrize("V", [100, 30_000, 90_000])
 def test_ids_outside_the_vocabulary_skip_the_row(V):
     import torch
