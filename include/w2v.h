@@ -541,7 +541,8 @@ int w2v_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx
  * scores, (id_k, t_k) the teacher's K entries and T the temperature:
  *   q   = softmax of t / T over the entries that are present,
  *   p_T = softmax(s / T), p_1 = softmax(s), both over all V words,
- *   loss = soft T^2 sum_k q_k (log q_k - log p_T(id_k)) - hard log p_1(label).
+ *   loss = soft T^2 sum_k q_k (log q_k - log p_T(id_k)) - hard log p_1(label),
+ * where a term of weight soft = 0 or hard = 0 is left out.
  *   logits     device rows x V of `dtype`, stride ld; -inf masks a word;
  *   ids        device int32[rows][K]: words, -1 = absent entry (its logit is
  *              not looked at); a row may have none (no soft term). Entries of
@@ -561,9 +562,9 @@ int w2v_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx
  *              memory (same stride), not overlap them otherwise.
  * A row whose scores are all -inf has loss 0 and gradient 0. NaN or +inf
  * among a row's scores makes its loss and its whole gradient NaN, whatever
- * terms the row has; among its present teacher logits, its loss. A row with an
- * id or a label outside [-1, V) has loss 0 and gradient 0 and is recorded in
- * the device's error word. Sums, statistics and loss are held in
+ * terms the row has; among its present teacher logits, its soft term. A row
+ * with an id or a label outside [-1, V) has loss 0 and gradient 0 and is
+ * recorded in the device's error word. Sums, statistics and loss are held in
  * fp32; the gradient is rounded once. The same call gives the same bits.
  * Limits: 0 <= K <= W2V_MAX_TEACHER, temperature in [2^-20, 2^20], rows >= 0,
  * V >= 1. workspace: device, 256-byte aligned, at least

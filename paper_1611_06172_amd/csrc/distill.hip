@@ -143,7 +143,7 @@ __device__ __forceinline__ List list_of(const Ctx& c) {
 }
 
 struct Row {
-  bool some;       // lists a word whose logit is above -inf
+  bool some;       // has a soft term: lists a word whose logit is above -inf
   bool ok;         // every id is a word or -1
   int32_t label;   // or -1
   float weight;    // of the gradient
@@ -189,7 +189,7 @@ __device__ __forceinline__ Row read_list(const Ctx& c, int row, const List& l) {
   block_maxima(m, fault, l.scratch);
   if (fault == 1.0f) m = NAN;
   r.ok = fault < 2.0f;
-  r.some = m != -INFINITY;
+  r.some = m != -INFINITY && c.a.soft != 0.0f;
   r.max = m;
   float sum = 0.0f;
   for (int k = tid; k < c.a.K; k += step)
@@ -243,7 +243,8 @@ __device__ __forceinline__ void write_loss(const Ctx& c, int row, const Row& r, 
   v = block_sum(v, l.scratch);
   if (threadIdx.x == 0) {
     float loss = c.a.soft * c.a.temperature * c.a.temperature * v;
-    if (live && r.label >= 0) loss += c.a.hard * (log_hard - (l.s[c.a.K] - s.max));
+    if (live && r.label >= 0 && c.a.hard != 0.0f)  // 0 times an infinite term is none
+      loss += c.a.hard * (log_hard - (l.s[c.a.K] - s.max));
     if (log_soft != log_soft) loss = NAN;  // whatever terms the row has
     if (!live) loss = 0.0f;
     c.a.loss[row] = loss;

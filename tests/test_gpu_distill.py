@@ -310,6 +310,31 @@ def test_nan_and_infinity_show_without_a_list(rows, V, T):
             assert torch.equal(out[key][good], want[key][good])
         assert torch.isfinite(back[good]).all()
 
+@pytest.mark.parametrize("V", [40, 9_000, 100_000])
+def test_term_without_weight_is_left_out(V):
+    """soft = 0 or hard = 0 takes the term out, also where it would be
+    infinite: a masked word that the teacher lists, a masked label."""
+    import torch
+    c = case(8, V, 5, "float32", V, masked=False)
+    z, ids = c["logits"], c["ids"]
+    z[3] = 0.5
+    ids[0, 0], ids[4, 1] = 2, 2
+    c["labels"][[0, 6]] = 2
+    z[[0, 4, 6], 2] = float("-inf")
+    kw = dict(temperature=2.0, want_grad=True)
+    none = torch.full_like(ids, -1)
+    a = w2v.distill_loss(z, ids, c["teacher"], labels=c["labels"], soft=0.0, hard=0.5, **kw)
+    b = w2v.distill_loss(z, none, c["teacher"], labels=c["labels"], soft=0.0, hard=0.5, **kw)
+    assert torch.equal(a["loss"], b["loss"]) and a["loss"][6] == float("inf")
+    keep = [r for r in range(8) if r != 6 and r != 0]
+    assert torch.isfinite(a["loss"][keep]).all() and torch.isfinite(a["grad"]).all()
+    a = w2v.distill_loss(z, ids, c["teacher"], labels=c["labels"], soft=0.7, hard=0.0, **kw)
+    b = w2v.distill_loss(z, ids, c["teacher"], soft=0.7, **kw)
+    # (row 0's word may be listed with a NaN)
+    assert torch.equal(a["loss"][1:], b["loss"][1:]) and torch.isfinite(a["grad"][1:]).all()
+    assert torch.isfinite(a["loss"][[1, 2, 3, 5, 6, 7]]).all()
+
+
 @pytest.mark.parametrize("V", [100, 30_000, 90_000])
 def test_ids_outside_the_vocabulary_skip_the_row(V):
     import torch
