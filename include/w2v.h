@@ -605,9 +605,9 @@ int w2v_distill_backward(const float* dloss, const void* logits, int64_t ld, int
  *             numbers are read;
  *   temperatures, top_ks, top_ps, min_ps  device arrays of `rows` settings,
  *             each NULL to use the scalar after it for every row.
- *             Temperature 0 takes the best-ranked word; top_k 0, top_p >= 1
- *             and min_p 0 are off; top_k is at most W2V_MAX_TOP_K, or >= V,
- *             which is off;
+ *             Temperature 0 takes the best-ranked word (others below 2^-126
+ *             act as 2^-126); top_k 0, top_p >= 1 and min_p 0 are off; top_k
+ *             is at most W2V_MAX_TOP_K, or >= V, which is off;
  *   ids       device int32[rows]; logprob device float[rows] or NULL: x - log
  *             sum of all w, the word's log-probability at T before the filters
  *             (0 at temperature 0).

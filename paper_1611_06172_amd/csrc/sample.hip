@@ -85,7 +85,8 @@ __device__ __forceinline__ Setting setting(const Ctx& c, int row) {
   s.ok = T >= 0.0f && T < INFINITY && p > 0.0f && least >= 0.0f && least <= 1.0f && k >= 0 &&
          (k <= W2V_MAX_TOP_K || k >= a.V);
   s.greedy = T == 0.0f;
-  s.inverse = 1.0f / T;
+  // kept finite, with its multiple by log2(e): a row's maximum is 0 times it
+  s.inverse = 1.0f / fmaxf(T, 0x1p-126f);
   s.k = k >= a.V ? 0 : k;
   s.p = p;
   s.floor = least > 0.0f ? logf(least) : -INFINITY;

@@ -152,6 +152,21 @@ def test_temperature_zero_takes_the_best():
         assert mixed["ids"][r] == (want[r] if r % 2 == 0 else ones["ids"][r])
 
 
+@pytest.mark.parametrize("rows,V", [(3, 700), (2, 20_000), (2, 100_000)])
+def test_smallest_temperatures_take_the_best(rows, V):
+    """Temperatures down to the least number above 0 leave the best word's
+    weight alone, whose log-probability is 0."""
+    import torch
+    z, u = scores(rows, V, "float32", V)
+    want = torch.argmax(z, dim=1).tolist()
+    for T in (1e-30, 1.2e-38, 5e-39, 1e-39, 1e-45):
+        for kw in (dict(), dict(top_k=9), dict(top_p=0.9), dict(min_p=0.5)):
+            for t in (T, torch.full((rows,), T, device="cuda")):
+                out = w2v.sample_words(z, u, temperature=t, **kw)
+                assert out["ids"].tolist() == want, (T, kw)
+                assert (out["logprob"] == 0).all()
+
+
 def test_settings_of_each_row():
     import torch
     z, u = scores(len(FILTERS), 30_000, "float32", 17)
