@@ -98,20 +98,24 @@ constexpr float kLog2e = 1.44269504088896341f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// erfc(|x|) by Abramowitz and Stegun, Handbook of Mathematical Functions
-// (1964), 7.1.26: a polynomial in 1 / (1 + p |x|) times exp(-x^2), within
-// 1.5e-7. A sixth of the library function's instructions.
+// erfc(|x|) as exp(-x^2) times a polynomial in t = 1 / (1 + p |x|), fitted to
+// exp(x^2) erfc(x) over [0, 10] for the least relative error: 4.3e-6, and about
+// as much from the argument's rounding. So the tail, where gelu is all of erfc,
+// is as exact as the rest. A sixth of the library function's instructions.
 __device__ __forceinline__ float erfc_of_abs(float x) {
   x = fabsf(x);
-  const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
+  const float t = __builtin_amdgcn_rcpf(1.0f + 0.435f * x);
   const float poly =
-      t * (0.254829592f +
-           t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+      t * (0.24592552f +
+           t * (0.23733466f +
+                t * (0.2734442f + t * (0.01285749f + t * (0.38129657f + t * -0.15085929f)))));
   return poly * exp2_fast(x * x * -kLog2e);
 }
 
 // FAST: with the hardware's exponential and reciprocal and the polynomial
-// above, for results that are rounded to 16 bits.
+// above, for results that are rounded to 16 bits: before that rounding they are
+// within 2e-5 of their value, 0.04 units of fp16 and 0.005 of bf16 (and bf16's
+// below 2^-126 may be 0).
 template <bool FAST>
 __device__ __forceinline__ float activate(float z, int activation) {
   switch (activation) {

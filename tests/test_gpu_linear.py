@@ -117,6 +117,28 @@ def test_whole_epilogue(M, N, K, name, out, activation):
     assert again.data_ptr() == r.data_ptr() and torch.equal(again, got)
 
 
+@pytest.mark.parametrize("activation", ["gelu", "silu", "tanh", "sigmoid"])
+@pytest.mark.parametrize("name", ["bfloat16", "float16"])
+def test_activations_at_every_16_bit_value(name, activation):
+    """z itself (a sum of one product by 1) at every value within 20: the
+    result is rounded once, half a unit, and what is rounded is within 2e-5 of
+    its value, 0.041 units of fp16. Both routes of the product."""
+    import torch
+    bits = torch.arange(-32768, 32768, dtype=torch.int32).to(torch.int16)
+    z = bits.view(dtype_of(name)).float()
+    z = z[z.abs() <= 20].to(dtype_of(name))
+    one = torch.ones((1, 1), dtype=z.dtype, device="cuda")
+    Z = z.double()
+    exact = act64(Z, activation)
+    digits, low = (8, 2.0 ** -126) if name == "bfloat16" else (11, 2.0 ** -24)
+    unit = 2.0 ** (torch.floor(torch.log2(exact.abs().clamp(min=1e-300))) - digits + 1)
+    bound = 0.55 * unit + (low if name == "bfloat16" else 0.55 * low)
+    for x, w in ((z.cuda()[:, None], one), (one, z.cuda()[:, None])):
+        got = w2v.linear(x, w, activation=activation).double().cpu().flatten()
+        worst = ((got - exact).abs() / bound).max().item()
+        assert worst <= 1.0, (worst, Z[((got - exact).abs() / bound).argmax()])
+
+
 @pytest.mark.parametrize("name", ["float32", "bfloat16"])
 @pytest.mark.parametrize("M,N,K", [(40, 70, 20_000), (33, 40, 9_001), (3, 33, 9_000)])
 def test_long_sum_is_split_and_joined(M, N, K, name):
