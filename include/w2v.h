@@ -55,7 +55,9 @@ extern "C" {
 #define W2V_ENOMEM (-3)      /* a host allocation failed */
 #define W2V_EUNSUPPORTED (-4)/* valid arguments outside the compiled shapes */
 #define W2V_EDEVICE_FLAG (-5)/* an earlier call skipped work for an id outside
-                                [0, V); nothing was launched by this call */
+                                [0, V), or rows of scores for an id, a label or
+                                a setting out of range; nothing was launched by
+                                this call */
 #define W2V_ENONFINITE (-6)  /* a loss bucket holds NaN or Inf (w2v_check_loss) */
 
 /* Shape limits of the compiled kernels. The HogBatch kernels keep all N
@@ -101,8 +103,9 @@ int w2v_init(void);
 
 /* Waits for `stream` (a hipStream_t; NULL is the null stream), then returns
  * W2V_EDEVICE_FLAG (and clears the error word) if a kernel of this library on
- * the current device skipped a minibatch for an id outside [0, V) since the
- * word was last reported, else W2V_OK. */
+ * the current device skipped a minibatch for an id outside [0, V), or a row of
+ * scores for an id, a label or a setting out of range, since the word was last
+ * reported, else W2V_OK. */
 int w2v_device_status(void* stream);
 
 /* Failure detection for training (not in the paper, which reports no loss):

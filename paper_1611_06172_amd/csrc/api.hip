@@ -41,8 +41,9 @@ static int hip_fail(hipError_t e, const char* what) {
 // Per-device state set up by w2v_init (or by the first GPU call on the
 // device): the error word, one int32 of pinned host memory mapped into the
 // device's address space. Kernels that skip a minibatch for an id outside
-// [0, V) store kStatusBadId into it (a system-scope store, so the host reads
-// it without a copy or a synchronisation); every later call on the device
+// [0, V) store kStatusBadId into it, those that skip a row of scores
+// kStatusBadRow (a system-scope store, so the host reads it without a copy or a
+// synchronisation; of several, the last); every later call on the device
 // reports it once as W2V_EDEVICE_FLAG and clears it.
 constexpr int kMaxDevices = 64;
 
@@ -118,8 +119,15 @@ static int enter_device(int32_t** status_dev, void** scratch_dev = nullptr,
   if (rc != W2V_OK) return rc;
   DeviceState& st = g_dev[dev];
   if (scratch_dev != nullptr) *scratch_dev = st.scratch;
-  if (*st.status_host != 0) {
+  const int32_t status = *st.status_host;
+  if (status != 0) {
     *st.status_host = 0;
+    if (status == kStatusBadRow)
+      return failf(W2V_EDEVICE_FLAG,
+                   "an earlier call on device %d skipped rows: a listed id or a label "
+                   "outside [-1, V), or a sampling setting out of range; this call "
+                   "launched nothing",
+                   dev);
     return failf(W2V_EDEVICE_FLAG,
                  "an earlier call on device %d skipped work: an id outside [0, V) "
                  "in the corpus, the negative table or a batch (stats[3] counts them); "

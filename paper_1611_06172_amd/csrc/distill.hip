@@ -251,7 +251,7 @@ __device__ __forceinline__ void write_loss(const Ctx& c, int row, const Row& r, 
     c.a.stats[(int64_t)row * 3] = s.max;
     c.a.stats[(int64_t)row * 3 + 1] = log_soft;
     c.a.stats[(int64_t)row * 3 + 2] = log_hard;
-    if (!r.ok) __hip_atomic_store(c.a.status, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+    if (!r.ok) report_row(c.a.status);
   }
 }
 
@@ -347,8 +347,7 @@ __global__ __launch_bounds__(kThreads) void k_gradient(Ctx c) {
   const int64_t lo = split * c.range;
   const int64_t hi = lo + c.range < c.a.V ? lo + c.range : c.a.V;
   const Row r = read_list<T>(c, row, l);
-  if (!r.ok && tid == 0)
-    __hip_atomic_store(c.a.status, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  if (!r.ok && tid == 0) report_row(c.a.status);
   const float* stats = c.a.stats + (int64_t)row * 3;
   const Slope g = begin_gradient(c, r, l, stats[0], stats[1], stats[2], lo, hi);
   const T* in = (const T*)c.a.logits + row * c.a.ld;

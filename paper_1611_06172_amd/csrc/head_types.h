@@ -6,7 +6,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "w2v.h"
+#include "w2v_internal.h"
 
 namespace w2v {
 
@@ -161,6 +161,11 @@ __device__ __forceinline__ float activation_slope(float z, int activation) {
     default:
       return 1.0f;
   }
+}
+
+// Records that a row was skipped for a list, a label or a setting out of range.
+__device__ __forceinline__ void report_row(int32_t* status) {
+  __hip_atomic_store(status, kStatusBadRow, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
 }
 
 // Reductions over a wavefront and over a block of up to 16 of them; every

@@ -586,7 +586,7 @@ __device__ void write_none(const Ctx& c, int row, const Setting& s) {
   if (threadIdx.x != 0) return;
   c.a.ids[row] = -1;
   if (c.a.logprob != nullptr) c.a.logprob[row] = NAN;
-  if (!s.ok) __hip_atomic_store(c.a.status, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  if (!s.ok) report_row(c.a.status);
 }
 // By one thread. sum: of all weights.
 __device__ __forceinline__ void write_word(const Ctx& c, int row, int32_t id, float x,

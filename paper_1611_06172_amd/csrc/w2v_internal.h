@@ -18,6 +18,9 @@ int ok();
 // device if needed, reports an earlier call's skipped work, and gives the
 // device address of the error word.
 int enter_call(int32_t** status_dev);
+// What a kernel stores in the error word for a row of scores whose list, label or
+// setting is out of range (beside device_common.h's kStatusBadId).
+constexpr int32_t kStatusBadRow = 2;
 // Records a HIP error (a hipError_t) and returns W2V_EHIP.
 int launch_failed(int hip_error, const char* what);
 

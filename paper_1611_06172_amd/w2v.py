@@ -221,8 +221,9 @@ def init():
 
 def device_status(stream=None):
     """Waits for the stream, then raises W2VError (code EDEVICE_FLAG) if a
-    kernel of the library skipped work for an id outside [0, V) since this
-    was last reported (w2v_device_status)."""
+    kernel of the library skipped work for an id outside [0, V), or a row of
+    scores for an id, a label or a setting out of range, since this was last
+    reported (w2v_device_status)."""
     _check(lib().w2v_device_status(_stream(stream)))
 
 

@@ -37,6 +37,37 @@ def test_example_learns_and_draws():
     assert (drawn["logprob"] <= 0).all() and torch.isfinite(drawn["logprob"]).all()
 
 
+def test_skipped_rows_are_reported_as_what_they_are():
+    """The error word tells a skipped row of scores from a skipped minibatch."""
+    import torch
+    z, u = torch.zeros((3, 50), device="cuda"), torch.rand((3, 50), device="cuda")
+    ids = torch.full((3, 2), -1, dtype=torch.int32, device="cuda")
+    t = torch.zeros((3, 2), device="cuda")
+    w2v.device_status()
+    one = torch.ones(3, device="cuda")
+
+    def text(call):
+        call()
+        with pytest.raises(w2v.W2VError) as err:
+            w2v.device_status()
+        assert err.value.code == w2v.EDEVICE_FLAG
+        w2v.device_status()
+        return str(err.value)
+
+    stats = w2v.distill_loss(z, ids, t)["stats"]
+    ids[1, 0] = 50
+    for call in (lambda: w2v.sample_words(z, u, temperature=-one),
+                 lambda: w2v.distill_loss(z, ids, t),
+                 lambda: w2v.distill_backward(one, z, ids, t, stats)):
+        message = text(call)
+        assert "skipped rows" in message and "setting" in message and "label" in message
+    words = torch.tensor([1, 2, 60], dtype=torch.int32, device="cuda")
+    M = torch.zeros((50, 32), device="cuda")
+    table = torch.arange(50, dtype=torch.int32, device="cuda")
+    message = text(lambda: w2v.train_epoch(words, M, M.clone(), table, window=1, K=2))
+    assert "corpus" in message
+
+
 def test_step_and_draw_replayed_from_a_graph():
     """Forward, distillation, backward and a draw, captured once and replayed
     on new inputs, with eager work between the replays."""
