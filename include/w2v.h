@@ -499,7 +499,7 @@ int w2v_step_batch_sorted(int32_t B, int32_t N, int32_t K, const int32_t* target
  *   dtype         type of x, W and pre (W2V_DTYPE_*);
  *   out_dtype     type of y and residual: dtype or W2V_DTYPE_F32;
  *   bias          device float[N] or NULL;
- *   residual      device M x N or NULL; may be y itself;
+ *   residual      device M x N or NULL; may be y itself (same stride);
  *   pre           device M x N or NULL: receives z = x W^T + b, which
  *                 w2v_linear_backward needs where there is an activation.
  * Sums and the epilogue are held in fp32 and each output is rounded once. The

@@ -113,6 +113,8 @@ int w2v_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, const flo
   if (residual != nullptr &&
       (rc = check_operand(residual, ldr, M, N, out_dtype, "residual")) != W2V_OK)
     return rc;
+  if (residual == y && ldr != ldy && M > 1)
+    return fail(W2V_EINVAL, "a residual in y's memory must have its stride");
   if (pre != nullptr && (rc = check_operand(pre, ldp, M, N, dtype, "pre")) != W2V_OK)
     return rc;
   if ((uintptr_t)bias % 4 != 0)

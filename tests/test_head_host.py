@@ -36,6 +36,14 @@ def test_linear_rejects(over, needle):
     refused(w2v.lib().w2v_linear, linear_args(**over), needle)
 
 
+def test_linear_residual_in_the_output_has_its_stride():
+    """Another stride over the same memory would read rows that are written."""
+    refused(w2v.lib().w2v_linear, linear_args(r=FAKE, ldr=6, ldy=5), "stride")
+    # as it is, the call gets as far as its workspace
+    refused(w2v.lib().w2v_linear, linear_args(r=FAKE, ldr=6, ldy=6, M=40, K=20_000,
+                                              ldx=20_000, ldw=20_000), "workspace must hold")
+
+
 def test_linear_too_many_tiles():
     big = 2**31 - 1
     refused(w2v.lib().w2v_linear, linear_args(M=big, N=big, ldr=big, ldy=big, ldp=big),
