@@ -598,7 +598,7 @@ hipError_t launch_type(const Ctx& c, bool forward, hipStream_t s) {
   return launch_as<T, kBoth>(c, forward, s);
 }
 
-hipError_t launch(const Ctx& c, bool forward, hipStream_t s) {
+hipError_t launch_part(const Ctx& c, bool forward, hipStream_t s) {
   switch (c.a.dtype) {
     case W2V_DTYPE_F32:
       return launch_type<float>(c, forward, s);
@@ -609,6 +609,27 @@ hipError_t launch(const Ctx& c, bool forward, hipStream_t s) {
   }
 }
 
+hipError_t launch(const DistillArgs& a, void* workspace, bool forward, hipStream_t s) {
+  const int most = rows_of_launch(a.rows);
+  hipError_t e = hipSuccess;
+  for (int64_t row = 0; row < a.rows && e == hipSuccess; row += most) {
+    DistillArgs part = a;
+    part.rows = (int32_t)(a.rows - row < most ? a.rows - row : most);
+    part.logits = row_at(a.logits, row, a.ld, a.dtype);
+    part.ids = row_at(a.ids, row, a.K);
+    part.teacher = row_at(a.teacher, row, a.K, a.teacher_dtype);
+    part.labels = row_at(a.labels, row);
+    part.row_weight = row_at(a.row_weight, row);
+    part.loss = row_at(a.loss, row);
+    part.stats = row_at(a.stats, row, 3);
+    part.grad = const_cast<void*>(row_at(a.grad, row, a.ldg, a.dtype));
+    Ctx c = context(part);
+    c.parts = (float*)workspace;
+    e = launch_part(c, forward, s);
+  }
+  return e;
+}
+
 }  // namespace
 
 size_t distill_workspace_bytes(int32_t rows, int32_t V, int32_t dtype) {
@@ -617,13 +638,11 @@ size_t distill_workspace_bytes(int32_t rows, int32_t V, int32_t dtype) {
 }
 
 hipError_t launch_distill(const DistillArgs& a, void* workspace, hipStream_t s) {
-  Ctx c = context(a);
-  c.parts = (float*)workspace;
-  return launch(c, true, s);
+  return launch(a, workspace, true, s);
 }
 
 hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t s) {
-  return launch(context(a), false, s);
+  return launch(a, nullptr, false, s);
 }
 
 }  // namespace w2v

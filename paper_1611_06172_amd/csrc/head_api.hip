@@ -39,7 +39,8 @@ int check_workspace(const void* workspace, size_t bytes, size_t need) {
   return W2V_OK;
 }
 
-int check_linear(int32_t M, int32_t N, int32_t K, int32_t dtype, int32_t activation) {
+int check_linear(int32_t M, int32_t N, int32_t K, int32_t dtype, int32_t activation,
+                 bool backward) {
   if (M < 0) return fail(W2V_EINVAL, "M must be >= 0");
   if (N < 1) return fail(W2V_EINVAL, "N must be positive");
   if (K < 1) return fail(W2V_EINVAL, "K must be positive");
@@ -52,6 +53,8 @@ int check_linear(int32_t M, int32_t N, int32_t K, int32_t dtype, int32_t activat
   const int64_t most = INT32_MAX / 64;
   if (m * n > most || m * k > most || n * k > most)
     return fail(W2V_EUNSUPPORTED, "the product has too many tiles");
+  if (!linear_fits(M, N, K, dtype, backward))
+    return fail(W2V_EUNSUPPORTED, "the product has too many tiles for a launch");
   return W2V_OK;
 }
 
@@ -94,7 +97,7 @@ using namespace w2v;
 extern "C" {
 
 size_t w2v_linear_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t dtype) {
-  if (check_linear(M, N, K, dtype, W2V_ACTIVATION_NONE) != W2V_OK) return 0;
+  if (check_linear(M, N, K, dtype, W2V_ACTIVATION_NONE, false) != W2V_OK) return 0;
   return linear_workspace_bytes(M, N, K, dtype);
 }
 
@@ -103,7 +106,7 @@ int w2v_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, const flo
                int64_t ldp, int32_t M, int32_t N, int32_t K, int32_t dtype,
                int32_t out_dtype, int32_t activation, void* workspace,
                size_t workspace_bytes, void* stream) {
-  int rc = check_linear(M, N, K, dtype, activation);
+  int rc = check_linear(M, N, K, dtype, activation, false);
   if (rc != W2V_OK) return rc;
   if (out_dtype != dtype && out_dtype != W2V_DTYPE_F32)
     return fail(W2V_EINVAL, "out_dtype must be dtype or W2V_DTYPE_F32");
@@ -150,7 +153,7 @@ int w2v_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, const flo
 
 size_t w2v_linear_backward_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t dtype,
                                            int32_t activation) {
-  if (check_linear(M, N, K, dtype, activation) != W2V_OK) return 0;
+  if (check_linear(M, N, K, dtype, activation, true) != W2V_OK) return 0;
   return linear_backward_workspace_bytes(M, N, K, dtype, activation);
 }
 
@@ -159,7 +162,7 @@ int w2v_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx
                         int64_t lddx, void* dw, int64_t lddw, float* db, int32_t M, int32_t N,
                         int32_t K, int32_t dtype, int32_t activation, void* workspace,
                         size_t workspace_bytes, void* stream) {
-  int rc = check_linear(M, N, K, dtype, activation);
+  int rc = check_linear(M, N, K, dtype, activation, true);
   if (rc != W2V_OK) return rc;
   if ((rc = check_operand(dy, lddy, M, N, dtype, "dy")) != W2V_OK) return rc;
   if ((rc = check_operand(x, ldx, M, K, dtype, "x")) != W2V_OK) return rc;

@@ -168,6 +168,21 @@ __device__ __forceinline__ void report_row(int32_t* status) {
   __hip_atomic_store(status, kStatusBadRow, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
 }
 
+// Rows of one launch of a block a row: a grid's threads, up to 1024 a row, are
+// counted in 32 bits. Calls with more rows are made of even parts.
+constexpr int kLaunchRows = 1 << 21;
+inline int rows_of_launch(int rows) {
+  const int parts = (rows + kLaunchRows - 1) / kLaunchRows;
+  return (rows + parts - 1) / parts;
+}
+inline const void* row_at(const void* p, int64_t row, int64_t ld, int32_t dtype) {
+  return p == nullptr ? p : (const char*)p + row * ld * (dtype == W2V_DTYPE_F32 ? 4 : 2);
+}
+template <typename V>
+inline V* row_at(V* p, int64_t row, int64_t ld = 1) {
+  return p == nullptr ? p : p + row * ld;
+}
+
 // Reductions over a wavefront and over a block of up to 16 of them; every
 // thread gets the result. `scratch`: 16 floats of LDS, free again on return.
 __device__ __forceinline__ float wave_sum(float v) {

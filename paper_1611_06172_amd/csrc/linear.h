@@ -32,6 +32,9 @@ struct LinearBackwardArgs {
   int32_t dtype, activation;
 };
 
+// Whether the product's blocks, or those of both gradients' products, fit a grid,
+// whose threads are counted in 32 bits.
+bool linear_fits(int32_t M, int32_t N, int32_t K, int32_t dtype, bool backward);
 size_t linear_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t dtype);
 size_t linear_backward_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t dtype,
                                        int32_t activation);

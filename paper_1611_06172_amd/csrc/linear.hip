@@ -4,6 +4,20 @@
 
 namespace w2v {
 
+bool linear_fits(int32_t M, int32_t N, int32_t K, int32_t dtype, bool backward) {
+  constexpr int64_t kMost = UINT32_MAX / 256;
+  if (M == 0) return true;
+  if (!backward && few_rows(M, K)) return ceil_div(N, 64) <= kMost;
+  // (the smallest tiles settle it for all but the largest outputs, and a product
+  // that is split has no more than kSlots blocks)
+  const int64_t m = ceil_div(M, 64), n = ceil_div(N, 64), k = ceil_div(K, 64);
+  if ((backward ? (m > n ? m : n) * k : m * n) <= kMost) return true;
+  auto blocks = [](const Plan& p) { return (int64_t)p.tiles_m * p.tiles_n * p.splits; };
+  if (!backward) return blocks(plan_product(M, N, K, dtype, false)) <= kMost;
+  const BackwardPlan b = plan_backward(M, N, K, dtype, W2V_ACTIVATION_NONE);
+  return blocks(b.dx) <= kMost && blocks(b.dw) <= kMost;
+}
+
 size_t linear_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t dtype) {
   if (M == 0 || few_rows(M, K)) return 0;
   return partial_bytes(plan_product(M, N, K, dtype, false), M, N) +

@@ -621,23 +621,27 @@ __global__ __launch_bounds__(kThreads) void k_slope_sums(const T* dy, int64_t ld
   }
 }
 
-// Adds up `parts` rows of N sums: 32 columns a block, every 32nd row a thread,
-// then the threads, in order.
+// Adds up `parts` rows of N sums: 32 columns a block at a time, every 32nd row a
+// thread, then the threads, in order.
 constexpr int kAdders = 32;
 __global__ __launch_bounds__(32 * kAdders) void k_add_rows(const float* in, int parts, int N,
                                                             float* out) {
   __shared__ float part[32 * kAdders];
-  const int tid = threadIdx.x, col = blockIdx.x * 32 + tid % 32;
-  float v = 0.0f;
-  if (col < N) {
+  const int tid = threadIdx.x;
+  for (int64_t first = blockIdx.x * 32; first < N; first += gridDim.x * 32) {
+    const int64_t col = first + tid % 32;
+    float v = 0.0f;
+    if (col < N) {
 #pragma unroll 8
-    for (int p = tid / 32; p < parts; p += kAdders) v += in[(int64_t)p * N + col];
-  }
-  part[tid] = v;
-  __syncthreads();
-  if (tid < 32 && col < N) {
-    for (int d = 1; d < kAdders; d++) v += part[d * 32 + tid];
-    out[col] = v;
+      for (int p = tid / 32; p < parts; p += kAdders) v += in[(int64_t)p * N + col];
+    }
+    part[tid] = v;
+    __syncthreads();
+    if (tid < 32 && col < N) {
+      for (int d = 1; d < kAdders; d++) v += part[d * 32 + tid];
+      out[col] = v;
+    }
+    __syncthreads();
   }
 }
 
@@ -646,11 +650,11 @@ __global__ __launch_bounds__(32 * kAdders) void k_add_rows(const float* in, int 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_copy(const T* in, int64_t ld, T* out, int64_t ldo,
                                                     int rows, int K) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
-  for (int col = (threadIdx.x & 63) * 8; col < K; col += 512) {
-    const uint4 v = load_end<T, 8>(in + row * ld + col, col + 8 - K, K);
-    __builtin_memcpy(out + row * ldo + col, &v, 16);
+  for (int64_t row = blockIdx.x * 4 + (threadIdx.x >> 6); row < rows; row += gridDim.x * 4) {
+    for (int col = (threadIdx.x & 63) * 8; col < K; col += 512) {
+      const uint4 v = load_end<T, 8>(in + row * ld + col, col + 8 - K, K);
+      __builtin_memcpy(out + row * ldo + col, &v, 16);
+    }
   }
 }
 
@@ -662,19 +666,24 @@ void align_rows(const void*& p, int64_t& ld, int rows, int K, void* copy, size_t
   if constexpr (sizeof(T) == 2) {
     if (bytes == 0 || ((uintptr_t)p % 64 == 0 && ld % 32 == 0)) return;
     const int64_t ldo = aligned_columns(K);
-    k_copy<T><<<(int)ceil_div(rows, 4), kThreads, 0, s>>>((const T*)p, ld, (T*)copy, ldo, rows, K);
+    const int64_t blocks = ceil_div(rows, 4), most = 1 << 23;  // threads fit 32 bits
+    k_copy<T><<<(int)(blocks < most ? blocks : most), kThreads, 0, s>>>((const T*)p, ld, (T*)copy,
+                                                                        ldo, rows, K);
     p = copy;
     ld = ldo;
   }
 }
 
-// Zeroes `bytes` bytes of each of `rows` rows, a wave a row.
+// Zeroes `bytes` bytes of each of `rows` rows, a wave a row at a time.
 __global__ __launch_bounds__(kThreads) void k_zero(char* p, int64_t stride, int rows,
                                                     int64_t bytes) {
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
-  for (int64_t i = threadIdx.x & 63; i < bytes; i += 64) p[row * stride + i] = 0;
+  for (int64_t row = blockIdx.x * 4 + (threadIdx.x >> 6); row < rows; row += gridDim.x * 4)
+    for (int64_t i = threadIdx.x & 63; i < bytes; i += 64) p[row * stride + i] = 0;
 }
+
+// Blocks of a kernel that goes on in steps of its grid, where `blocks` would do
+// all of its work at once.
+inline int grid_of(int64_t blocks) { return (int)(blocks < 65536 ? blocks : 65536); }
 
 // The kernel of the plan's tile.
 template <typename T, typename TO, bool AKC, bool BKC, bool FULL>
@@ -768,7 +777,8 @@ hipError_t launch_backward_as(const LinearBackwardArgs& l, void* workspace, hipS
           (const T*)l.dy, l.lddy, (const T*)l.pre, l.ldp, wants_dz ? (T*)ws : nullptr, l.M,
           l.N, l.activation, p.across, p.rows, p.chunks > 1 ? sums : l.db);
       if (p.chunks > 1)
-        k_add_rows<<<(int)ceil_div(l.N, 32), 32 * kAdders, 0, s>>>(sums, p.chunks, l.N, l.db);
+        k_add_rows<<<grid_of(ceil_div(l.N, 32)), 32 * kAdders, 0, s>>>(sums, p.chunks, l.N,
+                                                                       l.db);
     } else if (wants_dz) {
       const int64_t units = (int64_t)l.M * ceil_div(l.N, 16 / (int)sizeof(T));
       const int64_t blocks = ceil_div(units, kThreads);
@@ -789,8 +799,8 @@ hipError_t launch_backward_as(const LinearBackwardArgs& l, void* workspace, hipS
   if (e != hipSuccess) return e;
   if (l.M == 0) {  // no row: dW and db are sums of nothing
     if (l.dw != nullptr)
-      k_zero<<<(int)ceil_div(l.N, 4), kThreads, 0, s>>>((char*)l.dw, l.lddw * sizeof(T), l.N,
-                                                        l.K * (int64_t)sizeof(T));
+      k_zero<<<grid_of(ceil_div(l.N, 4)), kThreads, 0, s>>>(
+          (char*)l.dw, l.lddw * sizeof(T), l.N, l.K * (int64_t)sizeof(T));
     if (l.db != nullptr)
       k_zero<<<1, kThreads, 0, s>>>((char*)l.db, 0, 1, l.N * (int64_t)4);
     return hipGetLastError();

@@ -861,7 +861,7 @@ size_t sample_workspace_bytes(int32_t rows, int32_t V) {
   return row_by_block(rows, V) ? 0 : layout(rows, V).total;
 }
 
-hipError_t launch_sample(const SampleArgs& a, void* workspace, hipStream_t s) {
+static hipError_t launch_part(const SampleArgs& a, void* workspace, hipStream_t s) {
   Ctx c{};
   c.a = a;
   c.splits = splits_of(a.rows, a.V);
@@ -889,6 +889,25 @@ hipError_t launch_sample(const SampleArgs& a, void* workspace, hipStream_t s) {
     default:
       return launch_as<f16_t>(c, s);
   }
+}
+
+hipError_t launch_sample(const SampleArgs& a, void* workspace, hipStream_t s) {
+  const int most = rows_of_launch(a.rows);
+  hipError_t e = hipSuccess;
+  for (int64_t row = 0; row < a.rows && e == hipSuccess; row += most) {
+    SampleArgs part = a;
+    part.rows = (int32_t)(a.rows - row < most ? a.rows - row : most);
+    part.logits = row_at(a.logits, row, a.ld, a.dtype);
+    part.uniforms = row_at(a.uniforms, row, a.ldu);
+    part.temperatures = row_at(a.temperatures, row);
+    part.top_ks = row_at(a.top_ks, row);
+    part.top_ps = row_at(a.top_ps, row);
+    part.min_ps = row_at(a.min_ps, row);
+    part.ids = row_at(a.ids, row);
+    part.logprob = row_at(a.logprob, row);
+    e = launch_part(part, workspace, s);
+  }
+  return e;
 }
 
 }  // namespace w2v

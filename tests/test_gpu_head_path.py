@@ -68,6 +68,49 @@ def test_skipped_rows_are_reported_as_what_they_are():
     assert "corpus" in message
 
 
+def test_more_rows_than_a_grid_of_blocks_holds():
+    """Rows whose blocks' threads would pass 2^32: made in parts, each row as in
+    a call of its own neighbours."""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    rows, V = 8_400_001, 3
+    z = torch.randn((rows, V), generator=g, device="cuda")
+    ids = torch.randint(-1, V, (rows, 1), generator=g, device="cuda", dtype=torch.int32)
+    t = torch.randn((rows, 1), generator=g, device="cuda")
+    labels = torch.randint(-1, V, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    w = torch.rand(rows, generator=g, device="cuda")
+    ends = [slice(0, 1000), slice(rows // 2, rows // 2 + 1000), slice(rows - 1000, rows)]
+    out = w2v.distill_loss(z, ids, t, labels=labels, hard=0.5, row_weight=w, want_grad=True)
+    back = w2v.distill_backward(w, z, ids, t, out["stats"], labels=labels, hard=0.5)
+    lp = torch.log_softmax(z, 1)
+    both = torch.where(ids[:, 0] >= 0, 1.0, 0.0), torch.where(labels >= 0, 0.5, 0.0)
+    want = -(both[0] * torch.gather(lp, 1, ids.clamp(min=0).long())[:, 0]
+             + both[1] * torch.gather(lp, 1, labels.clamp(min=0).long()[:, None])[:, 0])
+    assert (out["loss"] - want).abs().max() <= 1e-5
+    for at in ends:
+        part = w2v.distill_loss(z[at], ids[at], t[at], labels=labels[at], hard=0.5,
+                                row_weight=w[at], want_grad=True)
+        assert all(torch.equal(part[k], out[k][at]) for k in part)
+        assert torch.equal(back[at], w2v.distill_backward(
+            w[at], z[at], ids[at], t[at], part["stats"], labels=labels[at], hard=0.5))
+    u = torch.rand((rows, V), generator=g, device="cuda")
+    k = torch.randint(0, 4, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    drawn = w2v.sample_words(z, u, temperature=w + 0.5, top_k=k, top_p=w + 0.2, min_p=w / 4)
+    for at in ends:
+        part = w2v.sample_words(z[at], u[at], temperature=w[at] + 0.5, top_k=k[at],
+                                top_p=w[at] + 0.2, min_p=w[at] / 4)
+        assert all(torch.equal(part[key], drawn[key][at]) for key in part)
+    assert (drawn["ids"] >= 0).all()
+    del z, u, out, back, drawn, lp
+    # and the gradients of no row over many words
+    n = 70_000_001
+    x = torch.empty((0, 1), dtype=torch.bfloat16, device="cuda")
+    wide = torch.empty((n, 1), dtype=torch.bfloat16, device="cuda")
+    none = w2v.linear_backward(torch.empty((0, n), dtype=torch.bfloat16, device="cuda"), x, wide)
+    assert (none["dw"] == 0).all() and (none["db"] == 0).all()
+
+
 def test_step_and_draw_replayed_from_a_graph():
     """Forward, distillation, backward and a draw, captured once and replayed
     on new inputs, with eager work between the replays."""

@@ -44,6 +44,18 @@ def test_linear_residual_in_the_output_has_its_stride():
                                               ldx=20_000, ldw=20_000), "workspace must hold")
 
 
+def test_linear_blocks_fit_a_grid():
+    """More blocks than a grid's 2^32 threads hold are refused, not launched;
+    a large output of 128 x 128 tiles is not among them."""
+    refused(w2v.lib().w2v_linear, linear_args(M=1, N=2**30 + 1, K=1, ldr=2**30 + 1,
+                                              ldy=2**30 + 1, ldp=2**30 + 1), "launch",
+            w2v.EUNSUPPORTED)
+    refused(w2v.lib().w2v_linear_backward, backward_args(M=2**31 - 64, N=5, K=3), "launch",
+            w2v.EUNSUPPORTED)
+    import torch
+    assert w2v.linear_workspace_bytes(1_000_000, 100_000, 300, torch.bfloat16) > 0
+
+
 def test_linear_too_many_tiles():
     big = 2**31 - 1
     refused(w2v.lib().w2v_linear, linear_args(M=big, N=big, ldr=big, ldy=big, ldp=big),
