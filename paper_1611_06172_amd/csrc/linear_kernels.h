@@ -86,14 +86,33 @@ __device__ __forceinline__ int granule_at(int r, int g) {
 
 // N elements at `at`, of which the last `past` are beyond the end of a row of
 // `length` and become 0. They are read 16 bytes up to the end and moved down: no
-// lane waits for single elements.
+// lane waits for single elements. They are moved by halves of words and by words,
+// not as one 128-bit number: a 64-bit shift whose amount lies in the last register
+// of a wave's allocation takes another amount on this GPU, and the compiler did
+// put it there.
 template <typename T, int N>
 __device__ __forceinline__ uint4 load_end(const T* at, int past, int length) {
   if (length < N) return __builtin_bit_cast(uint4, load_some<T, N>(at, N - past));
-  typedef unsigned __int128 u128;
-  u128 v = __builtin_bit_cast(u128, load_16(at - (past > 0 ? past : 0)));
-  v = past >= N ? 0 : past > 0 ? v >> (past * 8 * (int)sizeof(T)) : v;
-  return __builtin_bit_cast(uint4, v);
+  const int by = past > 0 ? past : 0;
+  const uint4 in = load_16(at - by);
+  uint32_t a = in.x, b = in.y, c = in.z, d = in.w;
+  int words = by;
+  if constexpr (sizeof(T) == 2) {
+    words = by >> 1;
+    const bool half = by & 1;
+    a = half ? a >> 16 | b << 16 : a;
+    b = half ? b >> 16 | c << 16 : b;
+    c = half ? c >> 16 | d << 16 : c;
+    d = half ? d >> 16 : d;
+  }
+  const bool one = words & 1, two = words & 2, all = by >= N;
+  a = one ? b : a;
+  b = one ? c : b;
+  c = one ? d : c;
+  d = one ? 0 : d;
+  a = two ? c : a;
+  b = two ? d : b;
+  return make_uint4(all ? 0 : a, all ? 0 : b, all || two ? 0 : c, all || two ? 0 : d);
 }
 
 // One operand's tile, ROWS rows by G granules of k, on its way through

@@ -23,6 +23,12 @@ BACKWARD = {
     (4_500, 300, 4_500, BF16): (2, False, 0, True, False),
     (4_099, 4_001, 72, BF16): (0, True, 0, True, True),
     (3_300, 3_203, 40, F16): (1, True, 0, True, True),
+    # sums over words whose last 16 bytes of a row hold 5, 6 and 7 of 8 elements
+    (600, 30_005, 513, BF16): (2, True, 2, False, False),
+    (1_942, 15_182, 363, F16): (2, True, 0, False, True),
+    (700, 20_007, 700, F16): (2, True, 2, False, False),
+    (9_621, 5_518, 70, BF16): (2, True, 1, True, True),
+    (47_089, 158, 87, BF16): (2, False, 0, True, False),
     (300, 4_100, 4_100, F32): (0, True, 2, False, False),
     (1_030, 9_001, 1_030, F32): (0, True, 1, False, False),
 }
