@@ -43,7 +43,8 @@ constexpr int kBounded = 256;
 typedef unsigned long long u64;
 
 struct Part {  // of one block's share of a row
-  float max, sum;
+  float max;
+  float rest;     // weights relative to max, but for one word at it
   float bound;    // a score that k of its words reach, or -inf
   int32_t first;  // lowest index of the maximum
   int32_t nan;
@@ -282,7 +283,7 @@ __device__ Part scan(const Ctx& c, int row, const Setting& s, int64_t lo, int64_
   p.nan = nan > 0.0f;
   p.best = 0;
   p.first = 0;
-  p.sum = 0.0f;
+  p.rest = 0.0f;
   p.bound = -INFINITY;
   if (s.bounded() && !s.greedy && s.ok) {
     const uint32_t key = sorted(key_of(m), blockDim.x, buffer);
@@ -301,8 +302,25 @@ __device__ Part scan(const Ctx& c, int row, const Setting& s, int64_t lo, int64_
   }
   if (s.greedy)
     p.first = (int32_t)~(uint32_t)block_best(m == max ? (u64)(uint32_t)~first : 0, wide);
-  else
-    p.sum = block_sum(m == -INFINITY ? 0.0f : sum * exp2_fast(x_of(m, max, scale)), scratch);
+  else {
+    float top = m == max ? sum : 0.0f;
+    p.rest = m == max || m == -INFINITY ? 0.0f : sum * exp2_fast(x_of(m, max, scale));
+    block_sums(top, p.rest, scratch);
+    if (top - 1.0f + p.rest < 0.25f && max < INFINITY) {
+      // The best word has nearly all of the weight, and beside it its thread's
+      // other words were rounded to units of 2^-24: they are added up again.
+      top = 0.0f;
+      if (m == max)
+        each_pack<T, 4>(logits_of<T>(c, row), lo, hi, [&](int32_t, const float(&v)[N], int) {
+#pragma unroll
+          for (int j = 0; j < N; j++)
+            top += v[j] == max ? 0.0f : exp2_fast((v[j] - max) * scale);
+        });
+      p.rest += block_sum(top, scratch);
+    } else {
+      p.rest += top - 1.0f;
+    }
+  }
   return p;
 }
 
@@ -588,11 +606,12 @@ __device__ void write_none(const Ctx& c, int row, const Setting& s) {
   if (c.a.logprob != nullptr) c.a.logprob[row] = NAN;
   if (!s.ok) report_row(c.a.status);
 }
-// By one thread. sum: of all weights.
+// By one thread. The sum of all weights is 1 + rest; rest by itself keeps the
+// log-probability of a nearly certain word as exact as any.
 __device__ __forceinline__ void write_word(const Ctx& c, int row, int32_t id, float x,
-                                           float sum) {
+                                           float rest) {
   c.a.ids[row] = id;
-  if (c.a.logprob != nullptr) c.a.logprob[row] = x - logf(sum);
+  if (c.a.logprob != nullptr) c.a.logprob[row] = x - log1pf(rest);
 }
 
 // A row by one block.
@@ -618,7 +637,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 2) void k_row(Ctx c)
   const float max = p.max;
   if (!s.ok || p.nan || !(max > -INFINITY)) return write_none(c, row, s);
   if (s.greedy) {
-    if (tid == 0) write_word(c, row, p.first, 0.0f, 1.0f);
+    if (tid == 0) write_word(c, row, p.first, 0.0f, 0.0f);
     return;
   }
   End end = {kBins, 0, 0, p.bound};
@@ -643,13 +662,14 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 2) void k_row(Ctx c)
   }
   if (tid == 0) {
     const int32_t id = (int32_t)~(uint32_t)best;
-    write_word(c, row, id, x_of(to_f32(logits_of<T>(c, row)[id]), max, s.inverse), p.sum);
+    write_word(c, row, id, x_of(to_f32(logits_of<T>(c, row)[id]), max, s.inverse), p.rest);
   }
 }
 
 // The row's maximum from its parts (a NaN in the row makes it NaN) and the sum
-// of its weights, in every thread; the parts are read by the wave's lanes.
-__device__ float row_max(const Ctx& c, int row, const Setting& s, float& sum, float& bound) {
+// of its weights but for one word at the maximum, in every thread; the parts are
+// read by the wave's lanes.
+__device__ float row_max(const Ctx& c, int row, const Setting& s, float& rest, float& bound) {
   const Part* parts = c.parts + (int64_t)row * c.splits;
   float m = -INFINITY, nan = 0.0f;
   bound = -INFINITY;  // k words of one share reach its bound, so the largest serves
@@ -661,11 +681,17 @@ __device__ float row_max(const Ctx& c, int row, const Setting& s, float& sum, fl
   m = wave_max(m);
   nan = wave_max(nan);
   bound = wave_max(bound);
-  sum = 0.0f;
-  for (int i = threadIdx.x & 63; i < c.splits; i += 64)
-    if (parts[i].max != -INFINITY)
-      sum += parts[i].sum * exp2_fast(x_of(parts[i].max, m, s.inverse * kLog2e));
-  sum = wave_sum(sum);
+  rest = 0.0f;
+  float tops = 0.0f;  // parts at the maximum
+  for (int i = threadIdx.x & 63; i < c.splits; i += 64) {
+    const bool top = parts[i].max == m;
+    tops += top ? 1.0f : 0.0f;
+    if (top)
+      rest += parts[i].rest;
+    else if (parts[i].max != -INFINITY)
+      rest += (1.0f + parts[i].rest) * exp2_fast(x_of(parts[i].max, m, s.inverse * kLog2e));
+  }
+  rest = wave_sum(rest) + (wave_sum(tops) - 1.0f);
   return nan > 0.0f ? NAN : m;
 }
 
@@ -702,8 +728,8 @@ __global__ __launch_bounds__(kThreads) void k_bins(Ctx c) {
   int64_t lo, hi;
   share_of(c, row, split, lo, hi);
   const Setting s = setting(c, row);
-  float sum, bound;
-  const float max = row_max(c, row, s, sum, bound);
+  float rest, bound;
+  const float max = row_max(c, row, s, rest, bound);
   if (!s.binned() || !(max > -INFINITY)) return;
   for (int i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
   __syncthreads();
@@ -723,8 +749,8 @@ __global__ __launch_bounds__(kThreads) void k_race(Ctx c) {
   int64_t lo, hi;
   share_of(c, row, split, lo, hi);
   const Setting s = setting(c, row);
-  float sum, bound;
-  const float max = row_max(c, row, s, sum, bound);
+  float rest, bound;
+  const float max = row_max(c, row, s, rest, bound);
   if (s.greedy || !s.ok || !(max > -INFINITY)) return;
   if (threadIdx.x == 0) count = 0;
   End end = {kBins, 0, 0, bound};
@@ -751,8 +777,8 @@ __global__ __launch_bounds__(THREADS, 8) void k_pick(Ctx c) {
   __shared__ End shared_end;
   const int row = blockIdx.x, tid = threadIdx.x;
   const Setting s = setting(c, row);
-  float sum, bound;
-  const float max = row_max(c, row, s, sum, bound);
+  float rest, bound;
+  const float max = row_max(c, row, s, rest, bound);
   if (!s.ok || !(max > -INFINITY)) return write_none(c, row, s);
   const Part* parts = c.parts + (int64_t)row * c.splits;
   u64 best = 0;
@@ -779,9 +805,9 @@ __global__ __launch_bounds__(THREADS, 8) void k_pick(Ctx c) {
   if (tid == 0) {
     const int32_t id = (int32_t)~(uint32_t)best;
     if (s.greedy)
-      write_word(c, row, id, 0.0f, 1.0f);
+      write_word(c, row, id, 0.0f, 0.0f);
     else
-      write_word(c, row, id, x_of(to_f32(logits_of<T>(c, row)[id]), max, s.inverse), sum);
+      write_word(c, row, id, x_of(to_f32(logits_of<T>(c, row)[id]), max, s.inverse), rest);
   }
 }
 

@@ -138,6 +138,33 @@ def test_equal_scores_are_ranked_by_index(V):
         assert ids[1:] == [0, 0, 0], (kw, ids)
 
 
+@pytest.mark.parametrize("name", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("rows,V", [(40, 300), (16, 20_000), (3, 100_003), (130, 66_000)])
+def test_log_probability_of_a_nearly_certain_word(rows, V, name):
+    """A word that has all but 1e-2 to 1e-9 of the weight: its log-probability
+    is -log(1 + the others' weight), to within that weight's own error: 128
+    additions, arguments of exp of two roundings, |x| up to 60, and a logarithm
+    of a few units: 300 units of 2^-24."""
+    import torch
+    g = torch.Generator()
+    g.manual_seed(V)
+    z = torch.randn((rows, V), generator=g) - 9 - math.log(V) - 10 * torch.rand(
+        (rows, 1), generator=g)
+    z[:, V // 3] = 0.75
+    z = z.to(getattr(torch, name))
+    u = torch.rand((rows, V), generator=g).cuda()
+    for T in (1.0, 0.8):
+        x = (z.double() - 0.75) / T
+        x[:, V // 3] = float("-inf")
+        exact = -torch.log1p(torch.exp(x).sum(dim=1))
+        for kw in (dict(top_k=1), dict(top_p=0.5), dict(min_p=0.9)):
+            out = w2v.sample_words(z.cuda(), u, temperature=T, **kw)
+            assert (out["ids"] == V // 3).all()
+            got = out["logprob"].double().cpu()
+            assert ((got - exact).abs() <= 300 * U * exact.abs()).all(), \
+                ((got - exact) / exact).abs().max() / U
+
+
 def test_temperature_zero_takes_the_best():
     import torch
     z, u = scores(9, 20_000, "bfloat16", 3)
