@@ -158,8 +158,8 @@ __device__ __forceinline__ float activation_slope(float z, int activation) {
       return p + z * p * q;
     }
     case W2V_ACTIVATION_TANH: {
-      const float t = tanhf(z);
-      return (1.0f - t) * (1.0f + t);
+      const float e = expf(-2.0f * fabsf(z));  // 1 - tanh^2 without cancellation
+      return 4.0f * e / ((1.0f + e) * (1.0f + e));
     }
     case W2V_ACTIVATION_SIGMOID:
       return (1.0f / (1.0f + expf(-z))) * (1.0f / (1.0f + expf(z)));

@@ -226,6 +226,31 @@ def test_bias_gradient_is_summed_before_dz_is_rounded(M, N, K, activation, name)
     rest = w2v.linear_backward(dy, x, w, activation=activation, pre=pre, want_db=False)
     assert torch.equal(rest["dx"], out["dx"]) and torch.equal(rest["dw"], out["dw"])
 
+@pytest.mark.parametrize("activation", ["silu", "tanh", "sigmoid"])
+def test_slopes_far_out(activation):
+    """act'(z) itself (dy = 1, a sum of one product by 1) for z within 20:
+    within 24 units of 2^-24 of its own size, however small: an exponential's
+    argument has one rounding, |z| <= 20 and a few steps follow. silu's, which
+    passes 0 near -1.28, of the larger of its two terms."""
+    import torch
+    z = torch.linspace(-20, 20, 4001, device="cuda")[:, None]
+    one = torch.ones((1, 1), device="cuda")
+    out = w2v.linear_backward(torch.ones_like(z), torch.ones_like(z), one,
+                              activation=activation, pre=z)
+    Z = z.double().cpu()
+    exact = slope64(Z, activation)
+    if activation == "tanh":
+        exact = 1 / torch.cosh(Z) ** 2
+    if activation == "sigmoid":
+        exact = torch.sigmoid(Z) * torch.sigmoid(-Z)
+    if activation == "silu":
+        exact = torch.sigmoid(Z) + Z * torch.sigmoid(Z) * torch.sigmoid(-Z)
+    size = exact.abs() if activation != "silu" else torch.maximum(
+        torch.sigmoid(Z), (Z * torch.sigmoid(Z) * torch.sigmoid(-Z)).abs())
+    worst = ((out["dx"].double().cpu() - exact).abs() / size).max().item() * 2.0 ** 24
+    assert worst <= 24, worst
+
+
 @pytest.mark.parametrize("name", ["float32", "bfloat16"])
 def test_backward_splits_long_sums(name):
     """dx sums over many words, dW and db over many rows: both split."""
