@@ -17,7 +17,9 @@ namespace {
 
 constexpr int kThreads = 512;
 
-// How p_1 is formed beside p_T.
+// How p_1 is formed beside p_T. Squaring for T = 1, 2, 4 and an exponential of its
+// own, us: 4,096 rows of 71,290 bf16 269, 268, 277 and 296 (259 without labels), fp32
+// 518, 529, 567 and 547; 65,536 of 1,000 bf16 90, 91, 93 and 96.
 constexpr int kSoftOnly = -1;  // not at all: no row has a label
 // 0, 1, 2: T is 1, 2 or 4, and exp(x) is exp(x / T) squared that often
 constexpr int kBoth = 3;  // any T: an exponential of its own
@@ -326,7 +328,10 @@ __device__ __forceinline__ Slope begin_gradient(const Ctx& c, const Row& r, cons
   return g;
 }
 
-// Replaces the entries' gradients. Entries of one word write the same value.
+// Replaces the entries' gradients. Entries of one word write the same value. Each
+// entry goes through the list, which outweighs the row where that is short and
+// the list long: 65,536 rows of 1,000 bf16 take 98 us with 16 entries, 134 with 64,
+// 756 with 256, 7,880 with 1,000.
 template <typename T, int MODE>
 __device__ void end_gradient(const Ctx& c, int row, const List& l, const Slope& g) {
   T* grad = (T*)c.a.grad + row * c.a.ldg;

@@ -347,12 +347,14 @@ __device__ __forceinline__ void tile_of(const ProductArgs& a, int& tm, int& tn, 
 // four on a CU. With one 256-wide block on it, a k of 300 is over before its
 // pipeline is full: bf16 4,096 x 71,290 x 300 617 us against 549 (both before
 // the loads lost their branch).
-// Measured, in traces: bf16 4,096 x 71,290 x 300 406 us and up (430 TFLOP/s,
-// output at 1.4 TB/s), its gradients with 8,191 rows 939 us (dx, 373 TFLOP/s)
-// and 861 (dW, 407); 65,536 x 300 x 300 with bias, gelu and residual 63; fp32
-// 512 x 10^6 x 300 2,650 (116 TFLOP/s, a library product of 8,192^3 has 153).
-// 16 bits are bound by what a CU waits for between memory, LDS and MFMA at a k
-// of ten tiles, fp32 by MFMA.
+// Measured, in traces: bf16 4,096 x 71,290 x 300 410 us and up (427 TFLOP/s,
+// output at 1.4 TB/s), its gradients with 8,191 rows 894 us and up (dx, 392
+// TFLOP/s) and 808 (dW, 434); 65,536 x 300 x 300 with bias, gelu and residual 62;
+// fp32 512 x 10^6 x 300 2,542 and up (121 TFLOP/s, a library product of 8,192^3
+// has 153). 16 bits are bound by waits: at a k of ten tiles the waves wait for
+// memory, LDS and each other in 54 to 66% of their cycles, while MFMA is busy in
+// 19 to 21% of the SIMDs' and LDS in 26 to 38% of the CUs'. fp32 is bound by
+// MFMA, busy in 78%.
 template <typename T, typename TO, bool AKC, bool BKC, bool FULL, int TM, int TN, int G,
           int PER_CU>
 __global__ __launch_bounds__(kThreads, PER_CU) void k_product(ProductArgs a) {
@@ -525,8 +527,8 @@ __global__ __launch_bounds__(kThreads) void k_join(ProductArgs a) {
 
 // Few rows of x (M <= 16): nothing of W is used twice, so W goes from memory
 // straight into MFMA registers, 16 of its rows a wave, with x's rows as the
-// other operand. Bound by W's bytes: 1 x 71,290 x 300 fp32 13.0 us in a trace,
-// 6.6 TB/s of which the memory-side cache holds a part from call to call.
+// other operand. Bound by W's bytes: 1 x 71,290 x 200 fp32 12.5 us in a trace,
+// 4.6 TB/s, k = 300 17.2 in a graph, 5.0.
 template <typename T, typename TO>
 __global__ __launch_bounds__(kThreads) void k_few_rows(ProductArgs a) {
   constexpr int GE = Matrix<T>::kGranule, STEP = 4 * GE, U = 4;

@@ -103,7 +103,8 @@ inline size_t copy_bytes(int32_t rows, int32_t M, int32_t N, int32_t K, int32_t 
 // Whether W is streamed past x (k_few_rows): at most 16 rows, one MFMA operand,
 // and a k that one wave goes through before tiles split along k would end.
 // Streamed and by tiles (us, in a graph): 1 x 71,290 x 300 fp32 17.5 and 38.5,
-// 16 rows 20.6 and 39.8; 1 x 10^6 x 300 bf16 122 and 152, 16 rows 187 and 172;
+// 16 rows 20.6 and 39.8; 1 x 10^6 x 300 bf16 122 and 152, 16 rows 187 and 172
+// (the one of these where streaming loses);
 // 1 x 4,096 x 2,000 fp32 28 and 33, bf16 9.7 and 11.5; 1 x 4,096 x 4,000 fp32
 // 55 and 34; 32 x 71,290 x 300 bf16 with two operands 17.9 and 14.9.
 inline bool few_rows(int32_t M, int32_t K) { return M <= 16 && K <= 2048; }

@@ -19,10 +19,14 @@
 // One block does all of them for a row of few words, or where there are enough
 // rows (k_row); otherwise each is a kernel over shares of the rows.
 // Bound by memory over many rows and by the chain of barriers over few. Measured
-// (us): 64 rows of 10^6 bf16 with top_p 187 (scan 26, bins 44, race 99: it reads
+// (us): 64 rows of 10^6 bf16 with top_p 187 (scan 25, bins 43, race 98: it reads
 // the kept words' random numbers one by one, pick 23), 0.7 TB/s of one reading of
 // the scores, which is read three times; 257 rows of 100,000 fp16 with top_k 50
-// 45 (1.1 TB/s, read twice); one row of 71,290 fp32 21 in three kernels.
+// 46 (1.1 TB/s, read twice); one row of 71,290 fp32 20 in three kernels.
+// Where the words that the end may cut are more than a list holds (nearly equal
+// scores), one block reads the whole row again, up to eight times: 64 rows of 10^6
+// scores within 1e-3 take 8,570 with top_p 0.9 and 1,780 with top_k 500, but 87 with
+// top_k 50; 64 rows of 60,000 199, 175 and 32.
 #include "sample.h"
 
 #include "head_types.h"
@@ -851,7 +855,10 @@ constexpr int kShortRow = 8192;
 // Whether a block does a whole row: short rows, or enough rows to fill the GPU,
 // fewer of them the shorter they are. By a block and by shares (us): 1 row of
 // 71,290 fp32 words, top_p, 48 and 34; 100 of 50,000 bf16 38 and 59; 257 of
-// 100,000 fp16 (top_k 50) 46 and 61; 64 of 10^6 bf16 (top_k 50) 112 and 69.
+// 100,000 fp16 (top_k 50) 46 and 61; 64 of 10^6 bf16 (top_k 50) 112 and 69. Below
+// the limit, one row of 8,192 fp32 words, top_p, 19 and 28, of 40,000 30 and 28, of
+// 65,536 39 and 29 (top_k 40 27 and 22); 64 rows of 40,000 34 and 50, of 65,536 45
+// and 63.
 bool row_by_block(int32_t rows, int32_t V) {
   return V <= 65536 || (rows >= 128 && V <= 131072) || rows >= 512;
 }
