@@ -352,9 +352,9 @@ __device__ __forceinline__ void tile_of(const ProductArgs& a, int& tm, int& tn, 
 // TFLOP/s) and 808 (dW, 434); 65,536 x 300 x 300 with bias, gelu and residual 62;
 // fp32 512 x 10^6 x 300 2,542 and up (121 TFLOP/s, a library product of 8,192^3
 // has 153). 16 bits are bound by waits: at a k of ten tiles the waves wait for
-// memory, LDS and each other in 54 to 66% of their cycles, while MFMA is busy in
-// 19 to 21% of the SIMDs' and LDS in 26 to 38% of the CUs'. fp32 is bound by
-// MFMA, busy in 78%.
+// memory, LDS and each other in 52 to 66% of their cycles, while MFMA is busy in
+// 19 to 21% of the SIMDs' (10% with the whole epilogue) and LDS in 26 to 38% of the
+// CUs'. fp32 is bound by MFMA, busy in 78%.
 template <typename T, typename TO, bool AKC, bool BKC, bool FULL, int TM, int TN, int G,
           int PER_CU>
 __global__ __launch_bounds__(kThreads, PER_CU) void k_product(ProductArgs a) {
