@@ -614,7 +614,6 @@ __global__ __launch_bounds__(kThreads) void k_slope_sums(const T* dy, int64_t ld
   const int m0 = blockIdx.y * rows, count = min(M - m0, rows);
   float total[V] = {};
   if (first < down && n > 0) {
-#pragma unroll 2
     for (int r = first; r < count; r += down) {
       const int64_t m = m0 + r;
       const Pack<T, V> g = load_some<T, V>(dy + m * lddy + col, n);
@@ -793,13 +792,15 @@ hipError_t launch_backward_as(const LinearBackwardArgs& l, void* workspace, hipS
   if (l.activation != W2V_ACTIVATION_NONE && l.M > 0) {
     const bool wants_dz = l.dx != nullptr || product;
     if (b.apart && l.db != nullptr) {
-      const SlopePlan& p = b.slope;
-      k_slope_sums<T><<<dim3(p.stripes, p.chunks), kThreads, 0, s>>>(
-          (const T*)l.dy, l.lddy, (const T*)l.pre, l.ldp, wants_dz ? (T*)ws : nullptr, l.M,
-          l.N, l.activation, p.across, p.rows, p.chunks > 1 ? sums : l.db);
-      if (p.chunks > 1)
-        k_add_rows<<<grid_of(ceil_div(l.N, 32)), 32 * kAdders, 0, s>>>(sums, p.chunks, l.N,
-                                                                       l.db);
+      if constexpr (sizeof(T) == 2) {
+        const SlopePlan& p = b.slope;
+        k_slope_sums<T><<<dim3(p.stripes, p.chunks), kThreads, 0, s>>>(
+            (const T*)l.dy, l.lddy, (const T*)l.pre, l.ldp, wants_dz ? (T*)ws : nullptr, l.M,
+            l.N, l.activation, p.across, p.rows, p.chunks > 1 ? sums : l.db);
+        if (p.chunks > 1)
+          k_add_rows<<<grid_of(ceil_div(l.N, 32)), 32 * kAdders, 0, s>>>(sums, p.chunks, l.N,
+                                                                         l.db);
+      }
     } else if (wants_dz) {
       const int64_t units = (int64_t)l.M * ceil_div(l.N, 16 / (int)sizeof(T));
       const int64_t blocks = ceil_div(units, kThreads);
