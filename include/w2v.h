@@ -56,7 +56,8 @@ extern "C" {
 #define W2V_EUNSUPPORTED (-4)/* valid arguments outside the compiled shapes */
 #define W2V_EDEVICE_FLAG (-5)/* an earlier call skipped work for an id outside
                                 [0, V), or rows of scores for an id, a label or
-                                a setting out of range; nothing was launched by
+                                a setting out of range, or rows for a word or a
+                                parent out of range; nothing was launched by
                                 this call */
 #define W2V_ENONFINITE (-6)  /* a loss bucket holds NaN or Inf (w2v_check_loss) */
 
@@ -635,6 +636,165 @@ int w2v_sample_words(const void* logits, int64_t ld, const float* uniforms, int6
                      const float* top_ps, float top_p, const float* min_ps, float min_p,
                      int32_t* ids, float* logprob, void* workspace, size_t workspace_bytes,
                      void* stream);
+
+/*
+ * A word model's ends: what brings words in and what answers with them, beside
+ * the vocabulary head. Matrices, element types and workspaces as there. (Not in
+ * the paper, which ends with the trained vectors.)
+ *
+ * Rows by word: y_i = scale W[id_i], for W V x D of `dtype` (M_in of a trained
+ * model) and y n x D of `out_dtype`, any of the types, rounded once.
+ *   ids       device int32[n]: words; -1 = absent, whose row of y is 0. Any
+ *             other id outside [0, V) gives a row of 0 too and is recorded in
+ *             the device's error word.
+ * y must not overlap any other argument. Limits: n >= 0, V >= 1,
+ * 1 <= D <= 2^24, scale finite.
+ */
+int w2v_embed(const int32_t* ids, int32_t n, const void* weight, int64_t ldw, int32_t V,
+              int32_t D, int32_t dtype, float scale, void* y, int64_t ldy, int32_t out_dtype,
+              void* stream);
+
+/*
+ * Gradient of w2v_embed for the weight, from dy (n x D of `dtype`):
+ *   grad[v] = scale sum of dy_i over the i with ids[i] = v, 0 for other words;
+ *   accumulate = 1: that is added to grad, whose other rows are not touched (a
+ *   negative scale makes it a step of gradient descent on the weight itself).
+ * grad is V x D of `grad_dtype`, any of the types. Ids as in w2v_embed; absent
+ * and out-of-range ones add nothing. Sums are held in fp32, over the positions
+ * sorted by word, in an order that depends on the ids alone, and each element is
+ * rounded once: the same call gives the same bits. workspace: device, 256-byte
+ * aligned, at least w2v_embed_backward_workspace_bytes(n, V, D) bytes (0 for n =
+ * 0), contents need not be initialised; calls that overlap in time must not
+ * share it. grad must not overlap any other argument.
+ */
+size_t w2v_embed_backward_workspace_bytes(int32_t n, int32_t V, int32_t D);
+int w2v_embed_backward(const void* dy, int64_t lddy, const int32_t* ids, int32_t n,
+                       int32_t dtype, float scale, void* grad, int64_t ldg, int32_t V, int32_t D,
+                       int32_t grad_dtype, int32_t accumulate, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/*
+ * Dropout: y = [r >= B] x 2^32 / (2^32 - B) + residual, B = floor(p 2^32 + 1/2),
+ * for x, residual and y rows x cols of `dtype`. The mask is not stored: the
+ * backward pass is the same call on dy (without the residual, whose gradient is
+ * dy). Element i = row cols + col (whatever the strides) has the 32-bit number
+ * r_i = 2^16 h_i + l_i; h and l are halves of words of Philox4x32-10 (Salmon et
+ * al., SC'11) with key (seed mod 2^32, seed / 2^32) and counter (b mod 2^32, b /
+ * 2^32 + 2^31 s, o mod 2^32, o / 2^32), b = i / 8, s = 0 for h and 1 for l: half
+ * i mod 8, a word's low half before its high one.
+ *   o          offset + *offset_dev, modulo 2^64: a different number for every
+ *              layer and step. offset_dev: device int64[1] or NULL (0), read by
+ *              the kernel, so that a captured graph gets new numbers as the
+ *              caller counts it up;
+ *   residual   or NULL (0); y may be x or the residual itself (same stride) and
+ *              must not overlap them otherwise.
+ * Whatever a dropped element holds (NaN, infinities) does not reach y. The
+ * product and the sum are rounded once, as one. p = 0 keeps and p = 1 drops
+ * everything. Limits: 0 <= p <= 1, rows >= 0, 1 <= cols <= 2^30.
+ */
+int w2v_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, void* y,
+                int64_t ldy, int32_t rows, int32_t cols, int32_t dtype, double p, uint64_t seed,
+                uint64_t offset, const int64_t* offset_dev, void* stream);
+
+/*
+ * A matrix in 4 bits. W (N x K) has G = ceil(K / group) groups of columns, group
+ * = 32, 64 or 128, and W_nk is held as scale_n,g (q - 8), q in [0, 15], with
+ * bfloat16 scales: scale = max |W| of the group / 7, rounded, and q = W / scale
+ * rounded to the nearest integer (even at ties), within [-8, 7], plus 8. A group
+ * with NaN or infinities becomes NaN.
+ * Layout: rows are in tiles of 16 (missing rows have q = 8 and scale 0), columns
+ * in B = G group / 32 blocks of 32 (missing ones have q = 8), which lie in fours,
+ * the rest (B mod 4) together:
+ *   packed  uint32[ceil(N / 16)][B * 64]: of blocks 4 i to 4 i + 3, word
+ *           [256 i + 4 l + j] is block 4 i + j's for lane l = 16 c + r, of the R
+ *           others word [256 (B / 4) + R l + j]; it holds row r of the tile,
+ *           columns 8 c to 8 c + 7 of the block: column 8 c + k in bits 2 k to 2
+ *           k + 3 for even k, 2 k + 14 to 2 k + 17 for odd k;
+ *   scales  bfloat16[ceil(N / 16)][G * 16]: of groups 4 i to 4 i + 3, [64 i + 4 r
+ *           + j] is group 4 i + j's for row r, of the R others [64 (G / 4) + R r +
+ *           j].
+ * packed is 16-byte aligned and of w2v_q4_packed_bytes bytes, scales of
+ * w2v_q4_scale_count elements (0 on invalid arguments). K <= 2^24.
+ */
+size_t w2v_q4_packed_bytes(int32_t N, int32_t K, int32_t group);
+size_t w2v_q4_scale_count(int32_t N, int32_t K, int32_t group);
+int w2v_quantize_q4(const void* w, int64_t ldw, int32_t N, int32_t K, int32_t dtype,
+                    int32_t group, void* packed, void* scales, void* stream);
+
+/*
+ * y = x W^T + bias for such a W, x M x K of `dtype` and y M x N of `out_dtype`
+ * (dtype or W2V_DTYPE_F32); bias: device float[N] or NULL. Made for few rows:
+ * the matrix is read once for every 64 of them (16-bit x) or 32 (fp32). Products
+ * are exact and sums fp32: of a group, sum x (q + 16) - 24 sum x, so x whose
+ * magnitudes add up to more than 2^122 in a group may overflow, and a row of x
+ * with an infinity gives NaN. Each output is rounded once; the same call gives
+ * the same bits. M = 0 is allowed and does nothing; M <= W2V_MAX_Q4_ROWS. y must
+ * not overlap any other argument.
+ */
+#define W2V_MAX_Q4_ROWS 1048576
+
+int w2v_linear_q4(const void* x, int64_t ldx, const void* packed, const void* scales,
+                  const float* bias, void* y, int64_t ldy, int32_t M, int32_t N, int32_t K,
+                  int32_t group, int32_t dtype, int32_t out_dtype, void* stream);
+
+/*
+ * A step of beam search over `batch` entries of `beams` beams each: of an entry's
+ * pairs (beam b, word v), the `width` with the largest scores_b + log p_b(v), p_b
+ * = softmax of row entry beams + b of the logits over all V words. Pairs of one
+ * beam are ranked by logit, equal ones by word; of different beams by the sum,
+ * formed in 64 bits from a sum of exponentials in fp32, equal ones by beam.
+ *   logits       device (batch * beams) x V of `dtype`, stride ld; -inf masks a
+ *                word;
+ *   scores       device float[batch][beams], a beam's log-probability so far;
+ *                -inf: the beam is none (a search starts with one beam per entry
+ *                at 0 and the others at -inf), and its logits are not read;
+ *   finished     device uint8[batch][beams] or NULL (none): a beam other than 0
+ *                has ended. It is one pair, (b, end) at its score, and its logits
+ *                are not read. Needs end >= 0;
+ *   end          the word that ends a beam, or -1;
+ *   words, parents  device int32[batch][width]: the pairs, best first; parents in
+ *                [0, beams). Where there are fewer pairs than width: -1, score
+ *                -inf;
+ *   new_scores   device float[batch][width];
+ *   new_finished device uint8[batch][width] or NULL: 1 where the parent had ended
+ *                or the word is end.
+ * An entry with a score of NaN or +inf, or with NaN or +inf among the logits of a
+ * beam that goes on, gets words and parents -1, scores NaN and flags 0. Outputs
+ * must not overlap any other argument. workspace: device, 256-byte aligned, at
+ * least w2v_beam_step_workspace_bytes bytes, contents need not be initialised;
+ * calls that overlap in time must not share it. Limits: 1 <= beams, width <=
+ * W2V_MAX_BEAMS, batch >= 0, V >= 1.
+ */
+#define W2V_MAX_BEAMS 64
+
+size_t w2v_beam_step_workspace_bytes(int32_t batch, int32_t beams, int32_t width, int32_t V,
+                                     int32_t dtype);
+int w2v_beam_step(const void* logits, int64_t ld, int32_t batch, int32_t beams, int32_t V,
+                  int32_t dtype, const float* scores, const uint8_t* finished, int32_t end,
+                  int32_t width, int32_t* words, int32_t* parents, float* new_scores,
+                  uint8_t* new_finished, void* workspace, size_t workspace_bytes, void* stream);
+
+/* A state of every beam: rows of row_bytes bytes (1 to W2V_MAX_STATE_BYTES), of
+ * any meaning and alignment, row strides in bytes. */
+typedef struct {
+  const void* src; /* device, batch * beams rows */
+  int64_t src_stride;
+  void* dst; /* device, batch * width rows */
+  int64_t dst_stride;
+  int64_t row_bytes;
+} w2v_beam_state;
+#define W2V_MAX_BEAM_STATES 16
+#define W2V_MAX_STATE_BYTES 17179869184 /* 2^34 */
+
+/*
+ * Moves states to where w2v_beam_step's pairs are: row entry width + j of dst is
+ * row entry beams + parents[entry][j] of src; a row of zeros where the parent is
+ * -1, or outside [-1, beams), which is recorded in the device's error word.
+ * states: host, `count` <= W2V_MAX_BEAM_STATES of them, read before the call
+ * returns. dst must not overlap any src.
+ */
+int w2v_beam_reorder(const w2v_beam_state* states, int32_t count, const int32_t* parents,
+                     int32_t batch, int32_t beams, int32_t width, void* stream);
 
 #ifdef __cplusplus
 }

@@ -20,7 +20,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 HIP_SOURCES = ["api.hip", "epoch_kernels.hip", "pairwise_kernels.hip",
                "step_kernels.hip", "step_sorted.hip", "vocab.hip", "radix_sort.hip",
                "head_api.hip", "linear.hip", "linear_f32.hip", "linear_bf16.hip",
-               "linear_f16.hip", "distill.hip", "sample.hip"]
+               "linear_f16.hip", "distill.hip", "sample.hip", "ends_api.hip",
+               "embed.hip", "dropout.hip", "linear_q4.hip", "beam.hip"]
 CXX_SOURCES = ["tables.cpp"]
 
 HIP_FLAGS = [

@@ -124,9 +124,9 @@ static int enter_device(int32_t** status_dev, void** scratch_dev = nullptr,
     *st.status_host = 0;
     if (status == kStatusBadRow)
       return failf(W2V_EDEVICE_FLAG,
-                   "an earlier call on device %d skipped rows: a listed id or a label "
-                   "outside [-1, V), or a sampling setting out of range; this call "
-                   "launched nothing",
+                   "an earlier call on device %d skipped rows: a listed id, a label "
+                   "or a word to embed outside [-1, V), a parent outside [-1, beams), or a "
+                   "sampling setting out of range; this call launched nothing",
                    dev);
     return failf(W2V_EDEVICE_FLAG,
                  "an earlier call on device %d skipped work: an id outside [0, V) "

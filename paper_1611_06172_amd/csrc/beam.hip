@@ -1,0 +1,482 @@
+// A step of beam search: of an entry's live beams b, with running scores c_b, and
+// the words v, the `width` pairs with the largest
+//
+//   c_b + log p_b(v) = (c_b - log sum exp z_b) + z_bv,
+//
+// and the beams' states moved to where their continuations are.
+//
+// The scores are read once. A row is cut into shares that one block holds in its
+// registers; the block writes the share's maximum and sum, and its `width` best
+// words, sorted. A second kernel, a block an entry, joins the sums and takes the
+// best of all shares' words. Words of one beam are ranked by their score, equal
+// ones by index, and no sum comes into that; pairs of different beams by the sum
+// above in 64 bits, equal ones by beam.
+//
+// The best words of a share lie above a bound that at least `width` of them reach:
+// the width-th largest of the maxima of 64 groups of four threads (of all 256
+// threads for wide beams). What reaches the bound goes to a list in LDS and is
+// ranked there by counting; if the list overflows (thousands of equal scores), the
+// words are taken one after the other.
+#include "beam.h"
+#include "head_types.h"
+
+namespace w2v {
+namespace {
+
+constexpr int kWave = 64;
+constexpr int kBlock = 256;
+constexpr int kWaves = kBlock / kWave;
+constexpr int kMaxGrid = 1 << 22;
+constexpr int kList = 1024;
+constexpr float kInf = __builtin_inff();
+
+__device__ __forceinline__ bool live_score(float c) { return c > -kInf; }  // not NaN
+
+// What a share leaves: {maximum, sum of exp(z - maximum)}, and `width` words.
+struct Share {
+  float most, sum;
+};
+struct Word {
+  float z;
+  int32_t id;
+};
+__device__ __forceinline__ bool better(const Word& a, const Word& b) {
+  return a.z > b.z || (a.z == b.z && a.id < b.id);
+}
+
+__device__ __forceinline__ Word best_of_wave(Word w) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    const Word o = {__shfl_xor(w.z, d), __shfl_xor(w.id, d)};
+    if (better(o, w)) w = o;
+  }
+  return w;
+}
+
+template <typename T, int PACKS>
+struct Row {
+  static constexpr int kE = 16 / (int)sizeof(T);
+  static constexpr int kShare = kBlock * PACKS * kE;
+  uint4 w[PACKS];
+
+  // Elements [first, first + kShare) of the n of a row; -inf past its end.
+  __device__ __forceinline__ void load(const T* row, int64_t first, int64_t n) {
+    const int64_t mine = first + threadIdx.x * kE;
+    if (first + kShare <= n) {
+#pragma unroll
+      for (int p = 0; p < PACKS; p++) w[p] = load_16(row + mine + p * kBlock * kE);
+      return;
+    }
+#pragma unroll
+    for (int p = 0; p < PACKS; p++) {
+      const int64_t i = mine + p * kBlock * kE;
+      if (i + kE <= n) {
+        w[p] = load_16(row + i);
+      } else {
+        Pack<T, kE> some;
+#pragma unroll
+        for (int e = 0; e < kE; e++) some.v[e] = i + e < n ? row[i + e] : from_f32<T>(-kInf);
+        w[p] = __builtin_bit_cast(uint4, some);
+      }
+    }
+  }
+  // f(score, index in the share), in order of the index
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) const {
+#pragma unroll
+    for (int p = 0; p < PACKS; p++) {
+      float z[kE];
+      unpack_words<T>(w[p], z);
+#pragma unroll
+      for (int e = 0; e < kE; e++) f(z[e], (p * kBlock + (int)threadIdx.x) * kE + e);
+    }
+  }
+};
+
+template <typename T, int PACKS>
+__global__ __launch_bounds__(kBlock) void k_beam_shares(BeamArgs a, int shares, Share* out,
+                                                        Word* best) {
+  __shared__ float s_most[kBlock];  // of groups of threads
+  __shared__ float s_wave[2 * kWaves];
+  __shared__ float s_bound;
+  __shared__ int s_count;
+  __shared__ Word s_list[kList];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t units = (int64_t)a.batch * a.beams * shares;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int64_t row = unit / shares;
+    // of an ended beam and of one that is none, nothing is read
+    if (a.finished != nullptr && a.finished[row] != 0) continue;
+    if (!live_score(a.scores[row])) continue;
+    const int64_t first = (unit - row * shares) * Row<T, PACKS>::kShare;
+    Row<T, PACKS> z;
+    z.load((const T*)a.logits + row * a.ld, first, a.V);
+    float most = -kInf;
+    z.each([&](float v, int) { most = fmaxf(most, v); });
+    const bool wide = a.width > 16;
+    float group = most;
+    if (!wide) {
+      group = fmaxf(group, __shfl_xor(group, 1));
+      group = fmaxf(group, __shfl_xor(group, 2));
+      if ((threadIdx.x & 3) == 0) s_most[threadIdx.x >> 2] = group;
+    } else {
+      s_most[threadIdx.x] = group;
+    }
+    const float of_wave = wave_max(group);
+    if (lane == 0) s_wave[wave] = of_wave;
+    if (threadIdx.x == 0) s_count = 0;
+    __syncthreads();
+    most = s_wave[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; w++) most = fmaxf(most, s_wave[w]);
+    // the width-th largest of the groups' maxima, by counting the larger ones
+    const int groups = wide ? kBlock : kBlock / 4;
+    if ((int)threadIdx.x < groups) {
+      const float mine = s_most[threadIdx.x];
+      int above = 0;
+      for (int i = 0; i < groups; i += 4) {
+        const f32x4 o = *(const f32x4*)(s_most + i);
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+          above += o[j] > mine || (o[j] == mine && i + j < (int)threadIdx.x) ? 1 : 0;
+      }
+      if (above == a.width - 1) s_bound = mine;
+    }
+    // a share of -inf alone has sum 0; NaN and +inf make it NaN
+    float sum = 0.0f;
+    const float top = most > -kInf ? most : 0.0f;
+    z.each([&](float v, int) { sum += exp2_fast((v - top) * kLog2e); });
+    sum = wave_sum(sum);
+    if (lane == 0) s_wave[kWaves + wave] = sum;
+    __syncthreads();
+    const float bound = s_bound;
+    z.each([&](float v, int i) {
+      if (v >= bound && v > -kInf) {
+        const int at = atomicAdd(&s_count, 1);
+        if (at < kList) s_list[at] = {v, i};
+      }
+    });
+    __syncthreads();
+    const int count = s_count;
+    Word* to = best + unit * a.width;
+    if (count <= kList) {
+      for (int i = threadIdx.x; i < count; i += kBlock) {
+        const Word mine = s_list[i];
+        int rank = 0;
+        for (int j = 0; j < count; j++) rank += better(s_list[j], mine) ? 1 : 0;
+        if (rank < a.width) to[rank] = {mine.z, (int32_t)(first + mine.id)};
+      }
+      for (int i = count + threadIdx.x; i < a.width; i += kBlock) to[i] = {-kInf, -1};
+    } else {
+      Word last = {kInf, -1};
+      for (int i = 0; i < a.width; i++) {
+        Word mine = {-kInf, 0x7fffffff};
+        z.each([&](float v, int id) {
+          if (v > mine.z && better(last, {v, id})) mine = {v, id};
+        });
+        mine = best_of_wave(mine);
+        __syncthreads();
+        if (lane == 0) s_list[wave] = mine;
+        __syncthreads();
+        last = s_list[0];
+#pragma unroll
+        for (int w = 1; w < kWaves; w++)
+          if (better(s_list[w], last)) last = s_list[w];
+        if (threadIdx.x == 0)
+          to[i] = {last.z, last.z > -kInf ? (int32_t)(first + last.id) : -1};
+      }
+    }
+    if (threadIdx.x == 0) {
+      sum = 0.0f;
+      for (int w = 0; w < kWaves; w++) sum += s_wave[kWaves + w];
+      out[unit] = {most, sum};
+    }
+    __syncthreads();
+  }
+}
+
+// A pair of beam and word, in the order in which they are taken.
+struct Pair {
+  double key;
+  float z;
+  int32_t beam, id;
+};
+__device__ __forceinline__ bool better(const Pair& a, const Pair& b) {
+  if (a.key != b.key) return a.key > b.key;
+  if (a.beam != b.beam) return a.beam < b.beam;
+  return a.z > b.z || (a.z == b.z && a.id < b.id);
+}
+
+__device__ __forceinline__ double wave_sum64(double v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+__global__ __launch_bounds__(kBlock) void k_beam_merge(BeamArgs a, int shares, const Share* share,
+                                                       const Word* best) {
+  __shared__ double s_add[W2V_MAX_BEAMS];     // what a beam's scores are added to
+  __shared__ uint8_t s_kind[W2V_MAX_BEAMS];   // 0: no word, 1: live, 2: ended
+  __shared__ int s_bad, s_count;
+  __shared__ Pair s_best[kBlock];
+  __shared__ Pair s_list[kList];
+  const Pair none = {-(double)kInf, -kInf, 0x7fffffff, 0x7fffffff};
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int64_t entry = blockIdx.x; entry < a.batch; entry += gridDim.x) {
+    if (threadIdx.x == 0) s_bad = s_count = 0;
+    __syncthreads();
+    for (int b = wave; b < a.beams; b += kWaves) {
+      const int64_t row = entry * a.beams + b;
+      const float c = a.scores[row];
+      int kind = 0;
+      double add = 0.0;
+      if (!(c < kInf)) {  // +inf or NaN
+        if (lane == 0) s_bad = 1;
+      } else if (c > -kInf && a.finished != nullptr && a.finished[row] != 0) {
+        kind = 2;
+        add = c;
+      } else if (c > -kInf) {
+        float most = -kInf;
+        for (int i = lane; i < shares; i += kWave) most = fmaxf(most, share[row * shares + i].most);
+        most = wave_max(most);
+        double sum = 0.0;
+        for (int i = lane; i < shares; i += kWave) {
+          const Share s = share[row * shares + i];
+          // of a share of -inf alone the sum is 0, or NaN if it holds one
+          sum += s.most > -kInf ? s.sum * exp((double)s.most - most) : (double)s.sum;
+        }
+        sum = wave_sum64(sum);
+        if (sum != sum || most == kInf) {
+          if (lane == 0) s_bad = 1;
+        } else if (most > -kInf) {
+          kind = 1;
+          add = (double)c - ((double)most + log(sum));
+        }
+      }
+      if (lane == 0) {
+        s_add[b] = add;
+        s_kind[b] = (uint8_t)kind;
+      }
+    }
+    __syncthreads();
+    const int64_t out = entry * a.width;
+    const auto write = [&](int i, const Pair& p, bool there) {
+      a.words[out + i] = there ? p.id : -1;
+      a.parents[out + i] = there ? p.beam : -1;
+      a.new_scores[out + i] = s_bad != 0 ? __builtin_nanf("") : (float)p.key;
+      if (a.new_finished != nullptr)
+        a.new_finished[out + i] = there && (s_kind[p.beam] == 2 || p.id == a.end) ? 1 : 0;
+    };
+    if (s_bad != 0) {
+      for (int i = threadIdx.x; i < a.width; i += kBlock) write(i, none, false);
+      __syncthreads();
+      continue;
+    }
+    // pair i: place i / lists of list i % lists, so that the lists' first ones
+    // are spread over the threads
+    const int lists = a.beams * shares;
+    const int pairs = lists * a.width;
+    const auto pair_of = [&](int i) {
+      const int place = i / lists, list = i - place * lists, b = list / shares;
+      Pair p = none;
+      if (s_kind[b] == 1) {
+        const Word w = best[(entry * lists + list) * a.width + place];
+        if (w.z > -kInf) p = {s_add[b] + (double)w.z, w.z, b, w.id};
+      } else if (s_kind[b] == 2 && place == 0 && list == b * shares) {
+        p = {s_add[b], 0.0f, b, a.end};
+      }
+      return p;
+    };
+    Pair mine = none;
+    for (int i = threadIdx.x; i < pairs; i += kBlock) {
+      const Pair p = pair_of(i);
+      if (better(p, mine)) mine = p;
+    }
+    s_best[threadIdx.x] = mine;
+    __syncthreads();
+    // the width-th best of the threads' best, by counting
+    int above = 0;
+    for (int i = 0; i < kBlock; i++)
+      above += better(s_best[i], mine) || (i < (int)threadIdx.x && !better(mine, s_best[i])) ? 1 : 0;
+    __syncthreads();
+    if (above == a.width - 1) s_best[0] = mine;
+    __syncthreads();
+    const Pair bound = s_best[0];
+    for (int i = threadIdx.x; i < pairs; i += kBlock) {
+      const Pair p = pair_of(i);
+      if (p.key > -(double)kInf && !better(bound, p)) {
+        const int at = atomicAdd(&s_count, 1);
+        if (at < kList) s_list[at] = p;
+      }
+    }
+    __syncthreads();
+    const int count = s_count;
+    if (count <= kList) {
+      for (int i = threadIdx.x; i < count; i += kBlock) {
+        const Pair p = s_list[i];
+        int rank = 0;
+        for (int j = 0; j < count; j++) rank += better(s_list[j], p) ? 1 : 0;
+        if (rank < a.width) write(rank, p, true);
+      }
+      for (int i = count + threadIdx.x; i < a.width; i += kBlock) write(i, none, false);
+    } else {
+      Pair last = {(double)kInf, 0.0f, 0, 0};
+      for (int n = 0; n < a.width; n++) {
+        mine = none;
+        for (int i = threadIdx.x; i < pairs; i += kBlock) {
+          const Pair p = pair_of(i);
+          if (p.key > -(double)kInf && better(last, p) && better(p, mine)) mine = p;
+        }
+        __syncthreads();
+        s_best[threadIdx.x] = mine;
+        __syncthreads();
+        if (wave == 0) {
+          for (int w = 1; w < kWaves; w++)
+            if (better(s_best[w * kWave + lane], mine)) mine = s_best[w * kWave + lane];
+          s_best[lane] = mine;
+        }
+        __syncthreads();
+        last = s_best[0];
+        for (int i = 1; i < kWave; i++)
+          if (better(s_best[i], last)) last = s_best[i];
+        if (threadIdx.x == 0) write(n, last, last.key > -(double)kInf);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------- reorder --
+
+constexpr int kChunk = 16;  // bytes
+constexpr int kAtOnce = 4;
+
+// Rows of every state (blockIdx.y) by parent, in chunks of 16 bytes, the last of a
+// row moved back to its end. An absent parent's row is 0 and reads nothing of its
+// own: the chunk of the entry's first beam is loaded and not used.
+__global__ __launch_bounds__(kBlock) void k_beam_reorder(ReorderArgs a) {
+  const w2v_beam_state st = a.states[blockIdx.y];
+  const int64_t per_row = (st.row_bytes + kChunk - 1) / kChunk;
+  const int64_t chunks = (int64_t)a.batch * a.width * per_row;
+  const bool whole = st.row_bytes >= kChunk;
+  constexpr int kStep = kBlock * kAtOnce;
+  for (int64_t base = (int64_t)blockIdx.x * kStep; base < chunks;
+       base += (int64_t)gridDim.x * kStep) {
+    const int64_t row0 = base / per_row, rest = base - row0 * per_row;
+    uint4 v[kAtOnce];
+    char* to[kAtOnce];
+    bool there[kAtOnce];
+    const char* from[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; u++) {
+      const int64_t i = rest + u * kBlock + threadIdx.x;
+      const bool some = base - rest + i < chunks;
+      const int64_t on = some ? divided((uint32_t)i, a.by_row[blockIdx.y]) : 0;
+      const int64_t row = row0 + on, entry = row / a.width;
+      const int64_t byte = some ? (i - on * per_row) * kChunk : 0;
+      const int64_t at = whole && byte + kChunk > st.row_bytes ? st.row_bytes - kChunk : byte;
+      const int32_t parent = a.parents[row];
+      there[u] = parent >= 0 && parent < a.beams;
+      if (!there[u] && parent != -1) report_row(a.status);
+      from[u] = (const char*)st.src + (entry * a.beams + (there[u] ? parent : 0)) * st.src_stride + at;
+      to[u] = some ? (char*)st.dst + row * st.dst_stride + at : nullptr;
+    }
+    if (whole) {
+#pragma unroll
+      for (int u = 0; u < kAtOnce; u++) v[u] = load_16(from[u]);
+#pragma unroll
+      for (int u = 0; u < kAtOnce; u++) {
+        if (to[u] == nullptr) continue;
+        if (!there[u]) v[u] = make_uint4(0, 0, 0, 0);
+        __builtin_memcpy(to[u], &v[u], 16);
+      }
+    } else {
+      for (int u = 0; u < kAtOnce; u++)
+        if (to[u] != nullptr)
+          for (int i = 0; i < (int)st.row_bytes; i++) to[u][i] = there[u] ? from[u][i] : 0;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ launch --
+
+// Packs a thread holds of a row: long shares leave fewer lists, short ones fill
+// the card.
+int packs_of(int64_t rows, int32_t V, int32_t dtype) {
+  const int64_t e = dtype == W2V_DTYPE_F32 ? 4 : 8;
+  for (int packs = 16; packs > 1; packs /= 4)
+    if (rows * ((V + kBlock * packs * e - 1) / (kBlock * packs * e)) >= 1024) return packs;
+  return 1;
+}
+
+int64_t share_count(int64_t rows, int32_t V, int32_t dtype) {
+  const int64_t of = (int64_t)kBlock * packs_of(rows, V, dtype) * (dtype == W2V_DTYPE_F32 ? 4 : 8);
+  return (V + of - 1) / of;
+}
+
+size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+template <typename T, int PACKS>
+void launch_shares(const BeamArgs& a, int shares, Share* share, Word* best, hipStream_t s) {
+  const int64_t units = (int64_t)a.batch * a.beams * shares;
+  const dim3 grid((unsigned)(units < kMaxGrid ? units : kMaxGrid));
+  hipLaunchKernelGGL((k_beam_shares<T, PACKS>), grid, dim3(kBlock), 0, s, a, shares, share, best);
+}
+
+template <typename T>
+void launch_shares(const BeamArgs& a, int shares, Share* share, Word* best, hipStream_t s) {
+  switch (packs_of((int64_t)a.batch * a.beams, a.V, a.dtype)) {
+    case 16:
+      return launch_shares<T, 16>(a, shares, share, best, s);
+    case 4:
+      return launch_shares<T, 4>(a, shares, share, best, s);
+    default:
+      return launch_shares<T, 1>(a, shares, share, best, s);
+  }
+}
+
+}  // namespace
+
+size_t beam_workspace_bytes(int32_t batch, int32_t beams, int32_t width, int32_t V,
+                            int32_t dtype) {
+  const int64_t rows = (int64_t)batch * beams;
+  const size_t lists = (size_t)(rows * share_count(rows, V, dtype));
+  return aligned(lists * sizeof(Share)) + aligned(lists * (size_t)width * sizeof(Word));
+}
+
+hipError_t launch_beam_step(const BeamArgs& a, void* workspace, hipStream_t s) {
+  const int64_t rows = (int64_t)a.batch * a.beams;
+  const int shares = (int)share_count(rows, a.V, a.dtype);
+  Share* share = (Share*)workspace;
+  Word* best = (Word*)((char*)workspace + aligned((size_t)rows * shares * sizeof(Share)));
+  switch (a.dtype) {
+    case W2V_DTYPE_F32:
+      launch_shares<float>(a, shares, share, best, s);
+      break;
+    case W2V_DTYPE_BF16:
+      launch_shares<bf16_t>(a, shares, share, best, s);
+      break;
+    default:
+      launch_shares<f16_t>(a, shares, share, best, s);
+  }
+  hipLaunchKernelGGL(k_beam_merge, dim3((unsigned)(a.batch < kMaxGrid ? a.batch : kMaxGrid)),
+                     dim3(kBlock), 0, s, a, shares, share, best);
+  return hipGetLastError();
+}
+
+hipError_t launch_beam_reorder(const ReorderArgs& args, hipStream_t s) {
+  ReorderArgs a = args;
+  int64_t most = 1;
+  for (int i = 0; i < a.count; i++) {
+    const int64_t per_row = (a.states[i].row_bytes + kChunk - 1) / kChunk;
+    const int64_t chunks = (int64_t)a.batch * a.width * per_row;
+    a.by_row[i] = divisor_of((uint32_t)per_row);
+    const int64_t blocks = (chunks + kBlock * kAtOnce - 1) / (kBlock * kAtOnce);
+    if (blocks > most) most = blocks;
+  }
+  const dim3 grid((unsigned)(most < (1 << 16) ? most : 1 << 16), (unsigned)a.count);
+  hipLaunchKernelGGL(k_beam_reorder, grid, dim3(kBlock), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace w2v

@@ -1,6 +1,6 @@
 // Element types, wide loads and stores, activations and launch helpers shared
-// by the kernels of the vocabulary head (linear.hip, distill.hip,
-// sample.hip).
+// by the kernels of the vocabulary head (linear.hip, distill.hip, sample.hip) and
+// of the model's ends (embed.hip, dropout.hip, linear_q4.hip, beam.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -92,6 +92,21 @@ __device__ __forceinline__ void store_some(T* p, int64_t n, const Pack<T, N>& v)
 #pragma unroll
   for (int i = 0; i < N; i++)
     if (i < n) p[i] = v.v[i];
+}
+
+// Division of a 32-bit number by a divisor that the host knows, as a product
+// (Granlund and Montgomery, PLDI'94): with 2^(shift-1) < d <= 2^shift,
+// n / d = (high(n m) + n) >> shift, exactly, for n below 2^31.
+struct Divisor {
+  uint32_t m, shift;
+};
+inline Divisor divisor_of(uint32_t d) {
+  uint32_t shift = 0;
+  while ((1ull << shift) < d) shift++;
+  return {(uint32_t)(((1ull << 32) * ((1ull << shift) - d)) / d + 1), shift};
+}
+__device__ __forceinline__ uint32_t divided(uint32_t n, Divisor d) {
+  return (__umulhi(n, d.m) + n) >> d.shift;
 }
 
 constexpr float kLog2e = 1.44269504088896341f;

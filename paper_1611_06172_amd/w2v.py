@@ -35,6 +35,12 @@ EDEVICE_FLAG = -5
 ENONFINITE = -6
 
 
+class _BeamState(ctypes.Structure):
+    """w2v_beam_state."""
+    _fields_ = [("src", _vp), ("src_stride", _i64), ("dst", _vp), ("dst_stride", _i64),
+                ("row_bytes", _i64)]
+
+
 class W2VError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"libw2v error {code}: {msg}")
@@ -126,6 +132,34 @@ def lib():
         _vp, _i64, _vp, _i64, _i32, _i32, _i32, _vp, _f32, _vp, _i32, _vp, _f32, _vp, _f32,
         _vp, _vp, _vp, ctypes.c_size_t, _vp]
     L.w2v_sample_words.restype = ctypes.c_int
+    L.w2v_embed.argtypes = [_vp, _i32, _vp, _i64, _i32, _i32, _i32, _f32, _vp, _i64, _i32, _vp]
+    L.w2v_embed.restype = ctypes.c_int
+    L.w2v_embed_backward_workspace_bytes.argtypes = [_i32, _i32, _i32]
+    L.w2v_embed_backward_workspace_bytes.restype = ctypes.c_size_t
+    L.w2v_embed_backward.argtypes = [
+        _vp, _i64, _vp, _i32, _i32, _f32, _vp, _i64, _i32, _i32, _i32, _i32, _vp,
+        ctypes.c_size_t, _vp]
+    L.w2v_embed_backward.restype = ctypes.c_int
+    L.w2v_dropout.argtypes = [
+        _vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _i32, _f64, _u64, _u64, _vp, _vp]
+    L.w2v_dropout.restype = ctypes.c_int
+    L.w2v_q4_packed_bytes.argtypes = [_i32, _i32, _i32]
+    L.w2v_q4_packed_bytes.restype = ctypes.c_size_t
+    L.w2v_q4_scale_count.argtypes = [_i32, _i32, _i32]
+    L.w2v_q4_scale_count.restype = ctypes.c_size_t
+    L.w2v_quantize_q4.argtypes = [_vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _vp]
+    L.w2v_quantize_q4.restype = ctypes.c_int
+    L.w2v_linear_q4.argtypes = [
+        _vp, _i64, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _i32, _i32, _i32, _i32, _vp]
+    L.w2v_linear_q4.restype = ctypes.c_int
+    L.w2v_beam_step_workspace_bytes.argtypes = [_i32, _i32, _i32, _i32, _i32]
+    L.w2v_beam_step_workspace_bytes.restype = ctypes.c_size_t
+    L.w2v_beam_step.argtypes = [
+        _vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp,
+        ctypes.c_size_t, _vp]
+    L.w2v_beam_step.restype = ctypes.c_int
+    L.w2v_beam_reorder.argtypes = [ctypes.POINTER(_BeamState), _i32, _vp, _i32, _i32, _i32, _vp]
+    L.w2v_beam_reorder.restype = ctypes.c_int
     _lib = L
     return L
 
@@ -221,9 +255,9 @@ def init():
 
 def device_status(stream=None):
     """Waits for the stream, then raises W2VError (code EDEVICE_FLAG) if a
-    kernel of the library skipped work for an id outside [0, V), or a row of
-    scores for an id, a label or a setting out of range, since this was last
-    reported (w2v_device_status)."""
+    kernel of the library skipped work for an id outside [0, V), a row of
+    scores for an id, a label or a setting out of range, or a row for a word or
+    a parent out of range, since this was last reported (w2v_device_status)."""
     _check(lib().w2v_device_status(_stream(stream)))
 
 
@@ -822,3 +856,278 @@ def sample_words(logits, uniforms=None, *, temperature=1.0, top_k=0, top_p=1.0, 
             _ptr(ids), _ptr(logprob), _ptr(ws), 0 if ws is None else ws.numel(),
             _stream(stream)))
     return dict(ids=ids, logprob=logprob)
+
+
+# ------------------------------------------------------- a word model's ends --
+
+def embed(ids, weight, *, scale: float = 1.0, out_dtype=None, out=None, stream=None):
+    """scale * weight[ids] (w2v_embed): (n, D) of out_dtype (weight's type by
+    default).
+
+    ids int32 (n,), -1 = absent, whose row is 0; weight (V, D) float32,
+    bfloat16 or float16, rows may be padded (a trained M_in of alloc_matrix is
+    one). out: receives the result."""
+    import torch
+    code = _head_dtype(weight, "weight")
+    ldw = _operand(weight, "weight")
+    V, D = weight.shape
+    _dev(ids, torch.int32, "ids", 1)
+    _here(ids, "ids")
+    n = ids.numel()
+    if out is not None:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError("out and out_dtype disagree")
+        out_dtype = out.dtype
+    out_dtype = weight.dtype if out_dtype is None else out_dtype
+    out_code = _dtypes().get(out_dtype)
+    if out_code is None:
+        raise TypeError(f"out_dtype must be float32, bfloat16 or float16, got {out_dtype}")
+    with _allocations(stream):
+        if out is None:
+            out = torch.empty((n, D), dtype=out_dtype, device=weight.device)
+        ldy = _operand(out, "out", (n, D), out_dtype)
+        _check(lib().w2v_embed(_ptr(ids), n, _ptr(weight), ldw, V, D, code, float(scale),
+                               _ptr(out), ldy, out_code, _stream(stream)))
+    return out
+
+
+def embed_backward_workspace_bytes(n: int, V: int, D: int) -> int:
+    return int(lib().w2v_embed_backward_workspace_bytes(n, V, D))
+
+
+def embed_backward(dy, ids, V: Optional[int] = None, *, scale: float = 1.0, grad=None,
+                   accumulate: bool = False, dtype=None, workspace=None, stream=None):
+    """Gradient of embed() for the weight from dy (n, D): rows of dy summed by
+    word, times scale (w2v_embed_backward).
+
+    A new (V, D) matrix of `dtype` (dy's by default), or `grad`, which is
+    overwritten or, with accumulate, added to at the words that occur: with a
+    negative scale that is a step of gradient descent on the weight itself."""
+    import torch
+    code = _head_dtype(dy, "dy")
+    lddy = _operand(dy, "dy")
+    n, D = dy.shape
+    _vector(ids, torch.int32, "ids", n)
+    if grad is not None:
+        if dtype is not None and grad.dtype != dtype:
+            raise TypeError("grad and dtype disagree")
+        if V is not None and grad.shape[0] != V:
+            raise ValueError("grad must have V rows")
+    elif V is None:
+        raise ValueError("V is needed without grad")
+    elif accumulate:
+        raise ValueError("accumulate needs grad")
+    with _allocations(stream):
+        if grad is None:
+            grad = torch.empty((V, D), dtype=dy.dtype if dtype is None else dtype,
+                               device=dy.device)
+        grad_code = _head_dtype(grad, "grad")
+        V = grad.shape[0]
+        ldg = _operand(grad, "grad", (V, D))
+        ws = _head_workspace(embed_backward_workspace_bytes(n, V, D), workspace, dy.device)
+        _check(lib().w2v_embed_backward(
+            _ptr(dy), lddy, _ptr(ids), n, code, float(scale), _ptr(grad), ldg, V, D, grad_code,
+            1 if accumulate else 0, _ptr(ws), 0 if ws is None else ws.numel(),
+            _stream(stream)))
+    return grad
+
+
+def dropout(x, p: float, *, seed: int, offset: int = 0, offset_dev=None, residual=None,
+            out=None, stream=None):
+    """x with each element dropped with probability p, the others over 1 - p,
+    plus the residual (w2v_dropout).
+
+    x (rows, cols) float32, bfloat16 or float16, rows may be padded. Which
+    elements are dropped follows from seed, offset (a different one for every
+    layer and step, both modulo 2^64) and an element's place alone: the
+    gradient is dropout(dy, p, ...) with the same ones. offset_dev: an int64
+    GPU tensor of one entry that the kernel adds to offset, for captured graphs.
+    out: receives the result (may be x or the residual itself)."""
+    import torch
+    code = _head_dtype(x, "x")
+    ldx = _operand(x, "x")
+    rows, cols = x.shape
+    ldr = cols if residual is None else _operand(residual, "residual", (rows, cols), x.dtype)
+    if offset_dev is not None:
+        _vector(offset_dev, torch.int64, "offset_dev", 1)
+    with _allocations(stream):
+        if out is None:
+            out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        ldy = _operand(out, "out", (rows, cols), x.dtype)
+        _check(lib().w2v_dropout(
+            _ptr(x), ldx, _ptr(residual), ldr, _ptr(out), ldy, rows, cols, code, float(p),
+            seed & 0xFFFFFFFFFFFFFFFF, offset & 0xFFFFFFFFFFFFFFFF, _ptr(offset_dev),
+            _stream(stream)))
+    return out
+
+
+def quantize_q4(weight, *, group: int = 32, stream=None):
+    """weight (N, K) in 4 bits with a bfloat16 scale for each `group` (32, 64 or
+    128) columns of a row (w2v_quantize_q4): a dict for linear_q4 of packed
+    (uint8) and scales (bfloat16), laid out as w2v.h says, shape (N, K) and
+    group."""
+    import torch
+    code = _head_dtype(weight, "weight")
+    ldw = _operand(weight, "weight")
+    N, K = weight.shape
+    with _allocations(stream):
+        packed = torch.empty(int(lib().w2v_q4_packed_bytes(N, K, group)), dtype=torch.uint8,
+                             device=weight.device)
+        scales = torch.empty(int(lib().w2v_q4_scale_count(N, K, group)), dtype=torch.bfloat16,
+                             device=weight.device)
+        _check(lib().w2v_quantize_q4(_ptr(weight), ldw, N, K, code, group, _ptr(packed),
+                                     _ptr(scales), _stream(stream)))
+    return dict(packed=packed, scales=scales, shape=(N, K), group=group)
+
+
+def linear_q4(x, weight, bias=None, *, out_dtype=None, out=None, stream=None):
+    """x W^T + bias for a W of quantize_q4() (w2v_linear_q4), which is read once
+    for every 64 rows of x (32 of float32).
+
+    x (M, K) float32, bfloat16 or float16, rows may be padded; bias float32
+    (N,). out_dtype: x's type (the default) or float32. out: receives the
+    result."""
+    import torch
+    code = _head_dtype(x, "x")
+    ldx = _operand(x, "x")
+    M, K = x.shape
+    N, group = weight["shape"][0], weight["group"]
+    if weight["shape"][1] != K:
+        raise ValueError("x and weight must have the same number of columns")
+    _vector(weight["packed"], torch.uint8, "packed", int(lib().w2v_q4_packed_bytes(N, K, group)))
+    _vector(weight["scales"], torch.bfloat16, "scales",
+            int(lib().w2v_q4_scale_count(N, K, group)))
+    if bias is not None:
+        _vector(bias, torch.float32, "bias", N)
+    if out is not None:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError("out and out_dtype disagree")
+        out_dtype = out.dtype
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    if out_dtype not in (x.dtype, torch.float32):
+        raise TypeError("out_dtype must be x's dtype or float32")
+    with _allocations(stream):
+        if out is None:
+            out = torch.empty((M, N), dtype=out_dtype, device=x.device)
+        ldy = _operand(out, "out", (M, N), out_dtype)
+        _check(lib().w2v_linear_q4(
+            _ptr(x), ldx, _ptr(weight["packed"]), _ptr(weight["scales"]), _ptr(bias), _ptr(out),
+            ldy, M, N, K, group, code, _dtypes()[out_dtype], _stream(stream)))
+    return out
+
+
+MAX_BEAMS = 64
+
+
+def beam_step_workspace_bytes(batch: int, beams: int, width: int, V: int, dtype) -> int:
+    return int(lib().w2v_beam_step_workspace_bytes(batch, beams, width, V, _dtypes()[dtype]))
+
+
+def beam_step(logits, scores, *, width: Optional[int] = None, finished=None, end: int = -1,
+              workspace=None, stream=None):
+    """The best `width` (as many as beams by default) continuations of each
+    entry's beams (w2v_beam_step): a dict of words and parents int32 (batch,
+    width), scores float32 (batch, width), best first, and finished uint8
+    (batch, width), or None without `end`.
+
+    logits (batch * beams, V) float32, bfloat16 or float16, rows may be padded,
+    -inf masks a word; scores float32 (batch, beams), a beam's log-probability
+    so far, -inf where there is none (at first: 0 and then -inf); finished uint8
+    (batch, beams): beams that have ended, which stay as they are; end: the word
+    that ends a beam. Places without a continuation get -1, -1 and -inf."""
+    import torch
+    code = _head_dtype(logits, "logits")
+    ld = _operand(logits, "logits")
+    _dev(scores, torch.float32, "scores", 2)
+    _here(scores, "scores")
+    batch, beams = scores.shape
+    rows, V = logits.shape
+    if rows != batch * beams:
+        raise ValueError("logits must have a row per score")
+    width = beams if width is None else width
+    if finished is not None:
+        _dev(finished, torch.uint8, "finished", 2)
+        _here(finished, "finished")
+        if finished.shape != scores.shape:
+            raise ValueError("finished must have the scores' shape")
+    dev = logits.device
+    with _allocations(stream):
+        need = int(lib().w2v_beam_step_workspace_bytes(batch, beams, width, V, code))
+        places = (batch, max(width, 0))
+        words = torch.empty(places, dtype=torch.int32, device=dev)
+        parents = torch.empty(places, dtype=torch.int32, device=dev)
+        new_scores = torch.empty(places, dtype=torch.float32, device=dev)
+        ended = torch.empty(places, dtype=torch.uint8, device=dev) if end != -1 else None
+        ws = _head_workspace(need, workspace, dev)
+        _check(lib().w2v_beam_step(
+            _ptr(logits), ld, batch, beams, V, code, _ptr(scores), _ptr(finished), end, width,
+            _ptr(words), _ptr(parents), _ptr(new_scores), _ptr(ended), _ptr(ws),
+            0 if ws is None else ws.numel(), _stream(stream)))
+    return dict(words=words, parents=parents, scores=new_scores, finished=ended)
+
+
+MAX_BEAM_STATES = 16
+
+
+def _state_rows(t, name):
+    """Bytes of a row of a state, and from one row to the next."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.dim() < 1:
+        raise ValueError(f"{name} must have a first dimension")
+    _here(t, name)
+    size = t.element_size()
+    rows = t.shape[0]
+    row = size
+    for n in t.shape[1:]:
+        row *= n
+    if t.is_contiguous():
+        return row, row
+    if not t[0].is_contiguous():
+        raise ValueError(f"{name} must have contiguous rows")
+    step = t.stride(0) * size
+    if rows > 1 and step < row:
+        raise ValueError(f"{name} must have rows that do not overlap")
+    return row, max(step, row)
+
+
+def beam_reorder(states, parents, *, out=None, stream=None):
+    """The beams' states where beam_step() has their continuations
+    (w2v_beam_reorder): row entry * width + j is row entry * beams +
+    parents[entry, j], zeros where the parent is -1.
+
+    states: a GPU tensor of batch * beams rows of any shape and type, or a list
+    of up to 16; parents int32 (batch, width). out: receives the result, in
+    states' form (not a state itself). Returns it in that form."""
+    import torch
+    one = isinstance(states, torch.Tensor)
+    states = [states] if one else list(states)
+    _dev(parents, torch.int32, "parents", 2)
+    _here(parents, "parents")
+    batch, width = parents.shape
+    if len(states) > MAX_BEAM_STATES:
+        raise ValueError(f"at most {MAX_BEAM_STATES} states")
+    beams = 1
+    with _allocations(stream):
+        if out is None:
+            new = [torch.empty((batch * width,) + tuple(t.shape[1:]), dtype=t.dtype,
+                               device=t.device) for t in states]
+        else:
+            new = [out] if one else list(out)
+            if len(new) != len(states):
+                raise ValueError("out must have a tensor per state")
+        table = (_BeamState * max(1, len(states)))()
+        for i, (t, o) in enumerate(zip(states, new)):
+            row, step = _state_rows(t, "states")
+            out_row, out_step = _state_rows(o, "out")
+            if o.dtype != t.dtype or o.shape != (batch * width,) + tuple(t.shape[1:]):
+                raise ValueError("out must have batch * width rows of the state's")
+            of = t.shape[0] // batch if batch else 1
+            if of * batch != t.shape[0] or of < 1 or (i > 0 and of != beams):
+                raise ValueError("states must have batch * beams rows each")
+            beams = of
+            table[i] = _BeamState(_ptr(t), step, _ptr(o), out_step, row)
+        _check(lib().w2v_beam_reorder(table, len(states), _ptr(parents), batch, beams, width,
+                                      _stream(stream)))
+    return new[0] if one else new
