@@ -13,8 +13,7 @@
 // above in 64 bits, equal ones by beam.
 //
 // The best words of a share lie above a bound that at least `width` of them reach:
-// the width-th largest of the maxima of 64 groups of four threads (of all 256
-// threads for wide beams). What reaches the bound goes to a list in LDS and is
+// the width-th largest of the maxima of groups of its threads. What reaches the bound goes to a list in LDS and is
 // ranked there by counting; if the list overflows (thousands of equal scores), the
 // words are taken one after the other.
 #include "beam.h"
@@ -41,7 +40,7 @@ struct Word {
   int32_t id;
 };
 __device__ __forceinline__ bool better(const Word& a, const Word& b) {
-  return a.z > b.z || (a.z == b.z && a.id < b.id);
+  return (a.z > b.z) | ((a.z == b.z) & (a.id < b.id));
 }
 
 __device__ __forceinline__ Word best_of_wave(Word w) {
@@ -52,6 +51,45 @@ __device__ __forceinline__ Word best_of_wave(Word w) {
   }
   return w;
 }
+
+// The n-th largest of the maxima of 64 groups of four threads, or of all threads'
+// values for n > 16, by counting the larger ones: what at least n values of the
+// block's threads reach. begin() and, behind a barrier, end() of all threads; the
+// result is there behind another one.
+struct Bound {
+  float groups[kBlock];
+  float waves[kWaves];
+
+  __device__ __forceinline__ static bool few(int n) { return n <= 16; }
+  __device__ __forceinline__ void begin(float v, int n) {
+    if (few(n)) {
+      v = fmaxf(v, __shfl_xor(v, 1));
+      v = fmaxf(v, __shfl_xor(v, 2));
+      if ((threadIdx.x & 3) == 0) groups[threadIdx.x >> 2] = v;
+    } else {
+      groups[threadIdx.x] = v;
+    }
+  }
+  __device__ __forceinline__ void end(int n) {
+    const int count = few(n) ? kBlock / 4 : kBlock;
+    if ((int)threadIdx.x >= count) return;
+    const float mine = groups[threadIdx.x];
+    int above = 0;
+#pragma unroll 8
+    for (int i = 0; i < count; i += 4) {
+      const f32x4 o = *(const f32x4*)(groups + i);
+      above += (o[0] > mine) + (o[1] > mine) + (o[2] > mine) + (o[3] > mine);
+    }
+    const float least = -wave_max(above < n ? -mine : -kInf);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = least;
+  }
+  __device__ __forceinline__ float get(int n) const {
+    float least = waves[0];
+    if (!few(n))
+      for (int w = 1; w < kWaves; w++) least = fminf(least, waves[w]);
+    return least;
+  }
+};
 
 template <typename T, int PACKS>
 struct Row {
@@ -80,6 +118,13 @@ struct Row {
       }
     }
   }
+  // Keeps the compiler from holding what one reading unpacked for the next: 8
+  // registers a pack instead of 4, and two wavefronts a SIMD instead of five.
+  __device__ __forceinline__ void repack() {
+#pragma unroll
+    for (int p = 0; p < PACKS; p++)
+      asm volatile("" : "+v"(w[p].x), "+v"(w[p].y), "+v"(w[p].z), "+v"(w[p].w));
+  }
   // f(score, index in the share), in order of the index
   template <typename F>
   __device__ __forceinline__ void each(F&& f) const {
@@ -87,8 +132,10 @@ struct Row {
     for (int p = 0; p < PACKS; p++) {
       float z[kE];
       unpack_words<T>(w[p], z);
+      int first = (int)threadIdx.x * kE;
+      asm volatile("" : "+v"(first));  // not an index for each element at once
 #pragma unroll
-      for (int e = 0; e < kE; e++) f(z[e], (p * kBlock + (int)threadIdx.x) * kE + e);
+      for (int e = 0; e < kE; e++) f(z[e], first + p * kBlock * kE + e);
     }
   }
 };
@@ -96,9 +143,8 @@ struct Row {
 template <typename T, int PACKS>
 __global__ __launch_bounds__(kBlock) void k_beam_shares(BeamArgs a, int shares, Share* out,
                                                         Word* best) {
-  __shared__ float s_most[kBlock];  // of groups of threads
+  __shared__ __attribute__((aligned(16))) Bound s_bound;
   __shared__ float s_wave[2 * kWaves];
-  __shared__ float s_bound;
   __shared__ int s_count;
   __shared__ Word s_list[kList];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -113,43 +159,25 @@ __global__ __launch_bounds__(kBlock) void k_beam_shares(BeamArgs a, int shares, 
     z.load((const T*)a.logits + row * a.ld, first, a.V);
     float most = -kInf;
     z.each([&](float v, int) { most = fmaxf(most, v); });
-    const bool wide = a.width > 16;
-    float group = most;
-    if (!wide) {
-      group = fmaxf(group, __shfl_xor(group, 1));
-      group = fmaxf(group, __shfl_xor(group, 2));
-      if ((threadIdx.x & 3) == 0) s_most[threadIdx.x >> 2] = group;
-    } else {
-      s_most[threadIdx.x] = group;
-    }
-    const float of_wave = wave_max(group);
+    s_bound.begin(most, a.width);
+    const float of_wave = wave_max(most);
     if (lane == 0) s_wave[wave] = of_wave;
     if (threadIdx.x == 0) s_count = 0;
     __syncthreads();
     most = s_wave[0];
 #pragma unroll
     for (int w = 1; w < kWaves; w++) most = fmaxf(most, s_wave[w]);
-    // the width-th largest of the groups' maxima, by counting the larger ones
-    const int groups = wide ? kBlock : kBlock / 4;
-    if ((int)threadIdx.x < groups) {
-      const float mine = s_most[threadIdx.x];
-      int above = 0;
-      for (int i = 0; i < groups; i += 4) {
-        const f32x4 o = *(const f32x4*)(s_most + i);
-#pragma unroll
-        for (int j = 0; j < 4; j++)
-          above += o[j] > mine || (o[j] == mine && i + j < (int)threadIdx.x) ? 1 : 0;
-      }
-      if (above == a.width - 1) s_bound = mine;
-    }
+    s_bound.end(a.width);
     // a share of -inf alone has sum 0; NaN and +inf make it NaN
+    z.repack();
     float sum = 0.0f;
     const float top = most > -kInf ? most : 0.0f;
     z.each([&](float v, int) { sum += exp2_fast((v - top) * kLog2e); });
     sum = wave_sum(sum);
     if (lane == 0) s_wave[kWaves + wave] = sum;
     __syncthreads();
-    const float bound = s_bound;
+    const float bound = s_bound.get(a.width);
+    z.repack();
     z.each([&](float v, int i) {
       if (v >= bound && v > -kInf) {
         const int at = atomicAdd(&s_count, 1);
@@ -163,13 +191,15 @@ __global__ __launch_bounds__(kBlock) void k_beam_shares(BeamArgs a, int shares, 
       for (int i = threadIdx.x; i < count; i += kBlock) {
         const Word mine = s_list[i];
         int rank = 0;
-        for (int j = 0; j < count; j++) rank += better(s_list[j], mine) ? 1 : 0;
+#pragma unroll 4
+        for (int j = 0; j < count; j++) rank += better(s_list[j], mine);
         if (rank < a.width) to[rank] = {mine.z, (int32_t)(first + mine.id)};
       }
       for (int i = count + threadIdx.x; i < a.width; i += kBlock) to[i] = {-kInf, -1};
     } else {
       Word last = {kInf, -1};
       for (int i = 0; i < a.width; i++) {
+        z.repack();
         Word mine = {-kInf, 0x7fffffff};
         z.each([&](float v, int id) {
           if (v > mine.z && better(last, {v, id})) mine = {v, id};
@@ -201,59 +231,62 @@ struct Pair {
   float z;
   int32_t beam, id;
 };
+// Without a branch, so that loops over it are unrolled with their loads in flight.
 __device__ __forceinline__ bool better(const Pair& a, const Pair& b) {
-  if (a.key != b.key) return a.key > b.key;
-  if (a.beam != b.beam) return a.beam < b.beam;
-  return a.z > b.z || (a.z == b.z && a.id < b.id);
-}
-
-__device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+  const bool word = (a.z > b.z) | ((a.z == b.z) & (a.id < b.id));
+  const bool beam = (a.beam < b.beam) | ((a.beam == b.beam) & word);
+  return (a.key > b.key) | ((a.key == b.key) & beam);
 }
 
 __global__ __launch_bounds__(kBlock) void k_beam_merge(BeamArgs a, int shares, const Share* share,
                                                        const Word* best) {
   __shared__ double s_add[W2V_MAX_BEAMS];     // what a beam's scores are added to
   __shared__ uint8_t s_kind[W2V_MAX_BEAMS];   // 0: no word, 1: live, 2: ended
-  __shared__ int s_bad, s_count;
-  __shared__ Pair s_best[kBlock];
+  __shared__ int s_bad, s_count, s_hot, s_lists[kList];
+  __shared__ __attribute__((aligned(16))) Bound s_bound;
+  __shared__ __attribute__((aligned(16))) double s_key[kList + 4];
+  // beam, word: the order of equal keys
+  __shared__ __attribute__((aligned(16))) uint64_t s_tie[kList + 4];
+  __shared__ __attribute__((aligned(16))) float s_z[kList + 4];
   __shared__ Pair s_list[kList];
   const Pair none = {-(double)kInf, -kInf, 0x7fffffff, 0x7fffffff};
+  int team = kWave;
+  while (team > 4 && team * a.beams > kBlock) team /= 2;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int64_t entry = blockIdx.x; entry < a.batch; entry += gridDim.x) {
-    if (threadIdx.x == 0) s_bad = s_count = 0;
+    if (threadIdx.x == 0) s_bad = s_count = s_hot = 0;
     __syncthreads();
-    for (int b = wave; b < a.beams; b += kWaves) {
-      const int64_t row = entry * a.beams + b;
+    // a beam's shares are joined by a team of lanes, all beams at once
+    for (int b0 = 0; b0 < a.beams; b0 += kBlock / team) {
+      const int b = b0 + (int)threadIdx.x / team, part = (int)threadIdx.x & (team - 1);
+      const int64_t row = entry * a.beams + (b < a.beams ? b : 0);
       const float c = a.scores[row];
-      int kind = 0;
-      double add = 0.0;
-      if (!(c < kInf)) {  // +inf or NaN
-        if (lane == 0) s_bad = 1;
-      } else if (c > -kInf && a.finished != nullptr && a.finished[row] != 0) {
-        kind = 2;
-        add = c;
-      } else if (c > -kInf) {
-        float most = -kInf;
-        for (int i = lane; i < shares; i += kWave) most = fmaxf(most, share[row * shares + i].most);
-        most = wave_max(most);
-        double sum = 0.0;
-        for (int i = lane; i < shares; i += kWave) {
+      const bool ended = a.finished != nullptr && a.finished[row] != 0;
+      const bool live = c > -kInf && c < kInf && !ended;
+      float most = -kInf;
+      double sum = 0.0;
+      if (live)
+        for (int i = part; i < shares; i += team) most = fmaxf(most, share[row * shares + i].most);
+      for (int d = team / 2; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+      if (live)
+        for (int i = part; i < shares; i += team) {
           const Share s = share[row * shares + i];
           // of a share of -inf alone the sum is 0, or NaN if it holds one
           sum += s.most > -kInf ? s.sum * exp((double)s.most - most) : (double)s.sum;
         }
-        sum = wave_sum64(sum);
-        if (sum != sum || most == kInf) {
-          if (lane == 0) s_bad = 1;
+      for (int d = team / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+      if (part == 0 && b < a.beams) {
+        int kind = 0;
+        double add = 0.0;
+        if (!(c < kInf) || sum != sum || most == kInf) {
+          s_bad = 1;  // +inf or NaN
+        } else if (c > -kInf && ended) {
+          kind = 2;
+          add = c;
         } else if (most > -kInf) {
           kind = 1;
           add = (double)c - ((double)most + log(sum));
         }
-      }
-      if (lane == 0) {
         s_add[b] = add;
         s_kind[b] = (uint8_t)kind;
       }
@@ -272,73 +305,130 @@ __global__ __launch_bounds__(kBlock) void k_beam_merge(BeamArgs a, int shares, c
       __syncthreads();
       continue;
     }
-    // pair i: place i / lists of list i % lists, so that the lists' first ones
-    // are spread over the threads
+    // Each list's words go to `ways` threads in turn (a thread has whole lists
+    // where there are more lists than threads), so a thread's best pair is the
+    // first of its first place.
     const int lists = a.beams * shares;
-    const int pairs = lists * a.width;
-    const auto pair_of = [&](int i) {
-      const int place = i / lists, list = i - place * lists, b = list / shares;
+    const int ways = lists < kBlock ? kBlock / lists : 1;
+    const int way = ways > 1 ? (int)threadIdx.x / lists : 0;
+    const int list0 = ways > 1 ? (int)threadIdx.x - way * lists : (int)threadIdx.x;
+    const int64_t list_base = entry * lists;
+    const auto pair_of = [&](int list, int place) {
+      const int b = list / shares;
       Pair p = none;
       if (s_kind[b] == 1) {
-        const Word w = best[(entry * lists + list) * a.width + place];
+        const Word w = best[(list_base + list) * a.width + place];
         if (w.z > -kInf) p = {s_add[b] + (double)w.z, w.z, b, w.id};
       } else if (s_kind[b] == 2 && place == 0 && list == b * shares) {
         p = {s_add[b], 0.0f, b, a.end};
       }
       return p;
     };
-    Pair mine = none;
-    for (int i = threadIdx.x; i < pairs; i += kBlock) {
-      const Pair p = pair_of(i);
-      if (better(p, mine)) mine = p;
-    }
-    s_best[threadIdx.x] = mine;
+    double first = -(double)kInf;
+    if (way < ways && way < a.width)
+      for (int list = list0; list < lists; list += kBlock) first = fmax(first, pair_of(list, way).key);
+    // in fp32: rounding keeps the keys' order, so no pair above the bound is lost
+    s_bound.begin((float)first, a.width);
     __syncthreads();
-    // the width-th best of the threads' best, by counting
-    int above = 0;
-    for (int i = 0; i < kBlock; i++)
-      above += better(s_best[i], mine) || (i < (int)threadIdx.x && !better(mine, s_best[i])) ? 1 : 0;
+    s_bound.end(a.width);
     __syncthreads();
-    if (above == a.width - 1) s_best[0] = mine;
+    // the lists that begin above the bound, then their words, all at once
+    const float bound = s_bound.get(a.width);
+    if (way == 0)
+      for (int list = list0; list < lists; list += kBlock) {
+        const Pair p = pair_of(list, 0);
+        if ((float)p.key >= bound && p.key > -(double)kInf) {
+          const int at = atomicAdd(&s_hot, 1);
+          if (at < kList) s_lists[at] = list;
+        }
+      }
     __syncthreads();
-    const Pair bound = s_best[0];
-    for (int i = threadIdx.x; i < pairs; i += kBlock) {
-      const Pair p = pair_of(i);
-      if (p.key > -(double)kInf && !better(bound, p)) {
-        const int at = atomicAdd(&s_count, 1);
-        if (at < kList) s_list[at] = p;
+    const int hot = s_hot;
+    for (int i = threadIdx.x; i < hot * a.width && hot <= kList; i += kBlock) {
+      const int at = i / a.width;
+      const Pair p = pair_of(s_lists[at], i - at * a.width);
+      if ((float)p.key >= bound && p.key > -(double)kInf) {
+        const int to = atomicAdd(&s_count, 1);
+        if (to < kList) {
+          s_list[to] = p;
+          s_key[to] = p.key;
+          s_tie[to] = (uint64_t)p.beam << 32 | (uint32_t)p.id;
+          s_z[to] = p.z;
+        }
       }
     }
     __syncthreads();
-    const int count = s_count;
+    const int count = hot <= kList ? s_count : kList + 1;
+    // pairs are compared in fours
+    if (count <= kList && threadIdx.x < 4) s_key[count + threadIdx.x] = none.key;
+    __syncthreads();
     if (count <= kList) {
-      for (int i = threadIdx.x; i < count; i += kBlock) {
-        const Pair p = s_list[i];
-        int rank = 0;
-        for (int j = 0; j < count; j++) rank += better(s_list[j], p) ? 1 : 0;
-        if (rank < a.width) write(rank, p, true);
+      // a pair's place by counting the better ones; few pairs have several threads.
+      // Scores of one beam that differ, but not in their keys, are rare: such a
+      // pair counts again by all that it is ranked by
+      int split = kWave;
+      while (split > 1 && split * count > kBlock) split /= 2;
+      for (int i0 = 0; i0 < count; i0 += kBlock / split) {
+        const int i = i0 + (int)threadIdx.x / split, part = (int)threadIdx.x & (split - 1);
+        const int at = i < count ? i : 0;
+        const double key = s_key[at];
+        const uint64_t tie = s_tie[at];
+        const float z = s_z[at];
+        int rank = 0, merged = 0;
+#pragma unroll 2
+        for (int j = part * 4; j < count; j += split * 4) {
+          const f32x4 zs = *(const f32x4*)(s_z + j);
+#pragma unroll
+          for (int u = 0; u < 4; u += 2) {
+            const double2 keys = *(const double2*)(s_key + j + u);
+            const ulonglong2 ties = *(const ulonglong2*)(s_tie + j + u);
+            const bool same0 = keys.x == key, same1 = keys.y == key;
+            rank += (keys.x > key) | (same0 & (ties.x < tie));
+            rank += (keys.y > key) | (same1 & (ties.y < tie));
+            merged |= same0 & (ties.x >> 32 == tie >> 32) & (zs[u] != z);
+            merged |= same1 & (ties.y >> 32 == tie >> 32) & (zs[u + 1] != z);
+          }
+        }
+        for (int d = split / 2; d > 0; d >>= 1) {
+          rank += __shfl_xor(rank, d);
+          merged |= __shfl_xor(merged, d);
+        }
+        if (part == 0 && i < count) {
+          const Pair p = s_list[i];
+          if (merged) {
+            rank = 0;
+            for (int j = 0; j < count; j++) rank += better(s_list[j], p);
+          }
+          if (rank < a.width) write(rank, p, true);
+        }
       }
       for (int i = count + threadIdx.x; i < a.width; i += kBlock) write(i, none, false);
     } else {
+      // one after the other: of each list the first pair behind the last taken
       Pair last = {(double)kInf, 0.0f, 0, 0};
       for (int n = 0; n < a.width; n++) {
-        mine = none;
-        for (int i = threadIdx.x; i < pairs; i += kBlock) {
-          const Pair p = pair_of(i);
-          if (p.key > -(double)kInf && better(last, p) && better(p, mine)) mine = p;
-        }
+        Pair mine = none;
+        if (way < ways)
+          for (int list = list0; list < lists; list += kBlock)
+            for (int place = way; place < a.width; place += ways) {
+              const Pair p = pair_of(list, place);
+              if (!(p.key > -(double)kInf)) break;
+              if (!better(last, p)) continue;
+              if (better(p, mine)) mine = p;
+              break;
+            }
         __syncthreads();
-        s_best[threadIdx.x] = mine;
+        s_list[threadIdx.x] = mine;
         __syncthreads();
         if (wave == 0) {
           for (int w = 1; w < kWaves; w++)
-            if (better(s_best[w * kWave + lane], mine)) mine = s_best[w * kWave + lane];
-          s_best[lane] = mine;
+            if (better(s_list[w * kWave + lane], mine)) mine = s_list[w * kWave + lane];
+          s_list[lane] = mine;
         }
         __syncthreads();
-        last = s_best[0];
+        last = s_list[0];
         for (int i = 1; i < kWave; i++)
-          if (better(s_best[i], last)) last = s_best[i];
+          if (better(s_list[i], last)) last = s_list[i];
         if (threadIdx.x == 0) write(n, last, last.key > -(double)kInf);
       }
     }
