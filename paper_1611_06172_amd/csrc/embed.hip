@@ -17,7 +17,6 @@
 // added by as many wavefronts as they take chunks, without atomics.
 #include "embed.h"
 #include "head_types.h"
-#include "kernel_args.h"
 
 namespace w2v {
 namespace {
@@ -65,6 +64,20 @@ __device__ __forceinline__ void put(T* p, int left, const Pack<T, kE>& v) {
   return store_pack<T, kE>(p, v);
 }
 
+// The same of a row that is read once, and of rows that are more than the caches
+// hold (`large`).
+template <bool SHORT, typename T>
+__device__ __forceinline__ Pack<T, kE> get_once(const T* p, int left) {
+  if constexpr (SHORT) return load_some<T, kE>(p, left);
+  return load_once<Pack<T, kE>>(p);
+}
+template <bool SHORT, typename T>
+__device__ __forceinline__ void put_once(T* p, int left, const Pack<T, kE>& v, bool large) {
+  if constexpr (SHORT) return store_some<T, kE>(p, left, v);
+  if (large) return store_once(p, v);
+  return store_pack<T, kE>(p, v);
+}
+
 // Column where pack `i` of a row begins.
 template <bool SHORT>
 __device__ __forceinline__ int pack_column(int i, int D) {
@@ -77,6 +90,9 @@ template <typename TI, typename TO, bool SHORT>
 __global__ __launch_bounds__(kBlock) void k_embed(EmbedArgs a, RowPacks p) {
   const TI* w = (const TI*)a.weight;
   TO* y = (TO*)a.y;
+  // rows of W stay in the L2s (32 MB) rather than y: 10^6 rows of 300 from 10^6,
+  // fp32 to bf16, in 206 us instead of 244 (4.1 to 4.9 TB/s past the L2s)
+  const bool large = (int64_t)a.n * a.D * (int64_t)sizeof(TO) > (32 << 20);
   for (int64_t b = (int64_t)blockIdx.x * p.rows_a_block; b < a.n;
        b += (int64_t)gridDim.x * p.rows_a_block) {
     const int rows = (int)(a.n - b < p.rows_a_block ? a.n - b : p.rows_a_block);
@@ -100,6 +116,8 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedArgs a, RowPacks p) {
         in[u] = get<SHORT>(w + (there ? id[u] : 0) * a.ldw + col[u], a.D - col[u]);
         if (!there) id[u] = -1;
       }
+      // every load is under way before the first is waited for
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int u = 0; u < 4; u++) {
         if (first + u * kBlock + (int)threadIdx.x >= packs) continue;
@@ -107,7 +125,7 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedArgs a, RowPacks p) {
 #pragma unroll
         for (int e = 0; e < kE; e++)
           out.v[e] = from_f32<TO>(id[u] >= 0 ? a.scale * to_f32(in[u].v[e]) : 0.0f);
-        put<SHORT>(y + (b + row[u]) * a.ldy + col[u], a.D - col[u], out);
+        put_once<SHORT>(y + (b + row[u]) * a.ldy + col[u], a.D - col[u], out, large);
       }
     }
   }
@@ -115,32 +133,66 @@ __global__ __launch_bounds__(kBlock) void k_embed(EmbedArgs a, RowPacks p) {
 
 // ------------------------------------------------------------- gradient --
 
-// Rows of zeros, in the packs of the block `b` of `grid`.
-template <typename T>
-__device__ __forceinline__ void clear_rows(T* g, int64_t ld, const RowPacks& p, int64_t b,
-                                           int64_t grid) {
-  Pack<T, kE> zero;
+// Rows of zeros, by bytes, which are 0 in every type: chunks of 16, the last of a
+// row moved back to its end.
+struct Clear {
+  char* rows;
+  int64_t ld;  // bytes
+  int32_t n, row_bytes, per_row, rows_a_block;
+  Divisor by_row;
+  int32_t blocks;        // 0: nothing to clear
+  const uint8_t* taken;  // rows that are written anyway, or NULL
+};
+
+__device__ __forceinline__ void clear_rows(const Clear& c, int64_t b) {
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  for (b *= c.rows_a_block; b < c.n; b += (int64_t)c.blocks * c.rows_a_block) {
+    const int rows = (int)(c.n - b < c.rows_a_block ? c.n - b : c.rows_a_block);
+    const int chunks = rows * c.per_row;
+    for (int first = threadIdx.x; first < chunks; first += 4 * (int)blockDim.x) {
+      int row[4], at[4];
+      bool taken[4];
 #pragma unroll
-  for (int e = 0; e < kE; e++) zero.v[e] = T(0.0f);
-  const bool whole = p.D >= kE;
-  for (b *= p.rows_a_block; b < p.n; b += grid * p.rows_a_block) {
-    const int rows = (int)(p.n - b < p.rows_a_block ? p.n - b : p.rows_a_block);
-    const int packs = rows * p.per_row;
-    for (int i = threadIdx.x; i < packs; i += (int)blockDim.x) {
-      const int row = (int)divided((uint32_t)i, p.by_row);
-      const int pack = i - row * p.per_row;
-      if (whole) {
-        store_pack<T, kE>(g + (b + row) * ld + pack_column<false>(pack, p.D), zero);
-      } else {
-        store_some<T, kE>(g + (b + row) * ld, p.D, zero);
+      for (int u = 0; u < 4; u++) {
+        const int i = first + u * (int)blockDim.x;
+        row[u] = (int)divided((uint32_t)(i < chunks ? i : first), c.by_row);
+        at[u] = ((i < chunks ? i : first) - row[u] * c.per_row) * 16;
+        taken[u] = i >= chunks || (c.taken != nullptr && c.taken[b + row[u]] != 0);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; u++) {
+        if (taken[u]) continue;
+        char* to = c.rows + (b + row[u]) * c.ld;
+        if (c.row_bytes >= 16) {
+          store_once(to + (at[u] + 16 <= c.row_bytes ? at[u] : c.row_bytes - 16), zero);
+        } else {
+          for (int j = 0; j < c.row_bytes; j += 2) *(uint16_t*)(to + j) = 0;
+        }
       }
     }
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kBlock) void k_embed_clear(T* g, int64_t ld, RowPacks p) {
-  clear_rows<T>(g, ld, p, blockIdx.x, gridDim.x);
+__global__ __launch_bounds__(kBlock) void k_embed_clear(Clear c) { clear_rows(c, blockIdx.x); }
+
+// Rows [first, last) of the gradient, if they are to be cleared, by blocks of
+// `threads`.
+Clear clear_of(const EmbedBackwardArgs& a, int64_t first, int64_t last, int threads = kBlock,
+               const uint8_t* taken = nullptr) {
+  Clear c{};
+  if (a.accumulate || first == last) return c;
+  const int64_t size = a.grad_dtype == W2V_DTYPE_F32 ? 4 : 2;
+  c.ld = a.ldg * size;
+  c.rows = (char*)a.grad + first * c.ld;
+  c.taken = taken == nullptr ? nullptr : taken + first;
+  c.n = (int32_t)(last - first);
+  c.row_bytes = (int32_t)(a.D * size);
+  c.per_row = (c.row_bytes + 15) / 16;
+  c.rows_a_block = c.per_row >= 4 * threads ? 1 : 4 * threads / c.per_row;
+  c.by_row = divisor_of((uint32_t)c.per_row);
+  const int64_t blocks = ((int64_t)c.n + c.rows_a_block - 1) / c.rows_a_block;
+  c.blocks = (int32_t)(blocks < kMaxGrid ? blocks : kMaxGrid);
+  return c;
 }
 
 // The sort's key of a word: itself, V where there is none.
@@ -150,54 +202,48 @@ __device__ __forceinline__ uint32_t word_key(int32_t id, int32_t V, int32_t* sta
   return (uint32_t)V;
 }
 
-__global__ __launch_bounds__(kBlock) void k_embed_keys(const int32_t* ids, int32_t n, int32_t V,
-                                                       uint32_t* keys, int32_t* status) {
-  const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-  if (i < n) keys[i] = word_key(ids[i], V, status);
-}
-
-// Up to kSortMax words sorted by one block, stably, by digits of six bits as in
-// radix_sort.hip, but with the elements in registers and the counters of a
-// wavefront's 64 digits in its 64 lanes: lane l counts digit l. Blocks after the
-// first clear the gradient meanwhile.
+// Up to 64 x 16 x GROUPS words sorted by one block, stably, by digits of six bits,
+// the elements in registers and the counters of a wavefront's 64 digits in its 64
+// lanes: lane l counts digit l. Blocks after the first clear the gradient
+// meanwhile.
 constexpr int kSortWaves = 16;
-constexpr int kSortGroups = 8;
-constexpr int kSortMax = kSortWaves * kSortGroups * kWave;  // 8,192
+constexpr int kSortMax = kSortWaves * 8 * kWave;  // 8,192
 
-// Lanes whose digit is d, from the ballots of the digits' six bits.
-__device__ __forceinline__ uint64_t lanes_with(const uint64_t (&set)[6], int d) {
+// Lanes whose digit is d, from the ballots of the digits' bits.
+template <int BITS>
+__device__ __forceinline__ uint64_t lanes_with(const uint64_t (&set)[BITS], int d) {
   uint64_t m = ~0ull;
 #pragma unroll
-  for (int b = 0; b < 6; b++) m &= (d >> b) & 1 ? set[b] : ~set[b];
+  for (int b = 0; b < BITS; b++) m &= (d >> b) & 1 ? set[b] : ~set[b];
   return m;
 }
 
-template <typename TG>
-__global__ __launch_bounds__(kSortWaves* kWave) void k_embed_sort(EmbedBackwardArgs a, int bits,
-                                                                uint32_t* keys, int32_t* at,
-                                                                RowPacks p) {
+template <int GROUPS>
+__global__ __launch_bounds__(kSortWaves* kWave) void k_embed_sort(
+    const int32_t* ids, int32_t n, int32_t V, int bits, uint32_t* keys, int32_t* at,
+    int32_t* status, Clear clear) {
   if (blockIdx.x > 0) {
-    clear_rows<TG>((TG*)a.grad, a.ldg, p, blockIdx.x - 1, gridDim.x - 1);
+    clear_rows(clear, blockIdx.x - 1);
     return;
   }
-  __shared__ uint32_t s_key[kSortMax];
-  __shared__ uint16_t s_at[kSortMax];
+  __shared__ uint32_t s_key[kSortWaves * GROUPS * kWave];
+  __shared__ uint16_t s_at[kSortWaves * GROUPS * kWave];
   __shared__ int s_count[kSortWaves * kWave];  // [digit][wave], then its start
   __shared__ int s_total[kSortWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t key[kSortGroups];
-  int from[kSortGroups];
+  uint32_t key[GROUPS];
+  int from[GROUPS];
 #pragma unroll
-  for (int g = 0; g < kSortGroups; g++) {
-    const int i = (wave * kSortGroups + g) * kWave + lane;
+  for (int g = 0; g < GROUPS; g++) {
+    const int i = (wave * GROUPS + g) * kWave + lane;
     from[g] = i;
     // past the end: behind everything, since the sort is stable
-    key[g] = i < a.n ? word_key(a.ids[i], a.V, a.status) : ~0u;
+    key[g] = i < n ? word_key(ids[i], V, status) : ~0u;
   }
   for (int shift = 0; shift < bits; shift += 6) {
-    int count = 0, rank[kSortGroups];
+    int count = 0, rank[GROUPS];
 #pragma unroll
-    for (int g = 0; g < kSortGroups; g++) {
+    for (int g = 0; g < GROUPS; g++) {
       const int d = (int)(key[g] >> shift) & 63;
       uint64_t set[6];
 #pragma unroll
@@ -217,11 +263,12 @@ __global__ __launch_bounds__(kSortWaves* kWave) void k_embed_sort(EmbedBackwardA
     }
     if (lane == kWave - 1) s_total[wave] = sum;
     __syncthreads();
-    for (int w = 0; w < wave; w++) sum += s_total[w];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; w++) sum += w < wave ? s_total[w] : 0;
     s_count[threadIdx.x] = sum - c;
     __syncthreads();
 #pragma unroll
-    for (int g = 0; g < kSortGroups; g++) {
+    for (int g = 0; g < GROUPS; g++) {
       const int d = (int)(key[g] >> shift) & 63;
       const int to = s_count[d * kSortWaves + wave] + rank[g];
       s_key[to] = key[g];
@@ -229,20 +276,186 @@ __global__ __launch_bounds__(kSortWaves* kWave) void k_embed_sort(EmbedBackwardA
     }
     __syncthreads();
 #pragma unroll
-    for (int g = 0; g < kSortGroups; g++) {
-      const int i = (wave * kSortGroups + g) * kWave + lane;
+    for (int g = 0; g < GROUPS; g++) {
+      const int i = (wave * GROUPS + g) * kWave + lane;
       key[g] = s_key[i];
       from[g] = s_at[i];
     }
-    __syncthreads();
   }
 #pragma unroll
-  for (int g = 0; g < kSortGroups; g++) {
-    const int i = (wave * kSortGroups + g) * kWave + lane;
-    if (i < a.n) {
+  for (int g = 0; g < GROUPS; g++) {
+    const int i = (wave * GROUPS + g) * kWave + lane;
+    if (i < n) {
       keys[i] = key[g];
       at[i] = from[g];
     }
+  }
+}
+
+// More words: passes over digits of up to ten bits, so that a vocabulary of up to
+// 2^20 words takes two. A block counts the digits of a tile of 2,048 words in LDS;
+// a wavefront a digit turns the tiles' counts into places; a block sends its tile
+// there in order. The gradient is cleared by further blocks of these launches,
+// which leave most of the card idle; the first one marks the rows that have words,
+// which are written later and need no zeros (10^6 words of 10^6, D 300: 17% of
+// them).
+constexpr int kDigitBits = 10;
+constexpr int kDigits = 1 << kDigitBits;
+constexpr int kTileGroups = 8;  // of a wavefront
+constexpr int kTileWaves = kBlock / kWave;
+constexpr int kTile = kTileWaves * kTileGroups * kWave;  // 2,048
+
+// A pass's keys: words (the first pass) or the pass before's.
+struct SortPass {
+  const int32_t* ids;  // or NULL
+  const uint32_t* keys;
+  const int32_t* at;
+  int32_t n, V, shift, digits, tiles;
+  int32_t* status;
+  uint8_t* taken;  // or NULL
+
+  __device__ __forceinline__ uint32_t key(int64_t i) const {
+    return ids != nullptr ? word_key(ids[i], V, status) : keys[i];
+  }
+  __device__ __forceinline__ int digit(uint32_t k) const { return (int)(k >> shift) & (digits - 1); }
+};
+
+__global__ __launch_bounds__(kBlock) void k_embed_count(SortPass p, int32_t* hist, Clear clear) {
+  if ((int)blockIdx.x >= p.tiles) {
+    clear_rows(clear, (int)blockIdx.x - p.tiles);
+    return;
+  }
+  __shared__ int s_count[kDigits];
+  for (int d = threadIdx.x; d < p.digits; d += kBlock) s_count[d] = 0;
+  const int64_t first = (int64_t)blockIdx.x * kTile + threadIdx.x;
+  uint32_t key[kTileGroups];
+#pragma unroll
+  for (int g = 0; g < kTileGroups; g++)
+    key[g] = first + g * kBlock < p.n ? p.key(first + g * kBlock) : 0;
+  __syncthreads();
+#pragma unroll
+  for (int g = 0; g < kTileGroups; g++)
+    if (first + g * kBlock < p.n) {
+      atomicAdd(&s_count[p.digit(key[g])], 1);
+      if (p.taken != nullptr && key[g] < (uint32_t)p.V) p.taken[key[g]] = 1;
+    }
+  __syncthreads();
+  for (int d = threadIdx.x; d < p.digits; d += kBlock)
+    hist[(int64_t)d * p.tiles + blockIdx.x] = s_count[d];
+}
+
+__device__ __forceinline__ int wave_prefix(int v, int lane) {
+#pragma unroll
+  for (int off = 1; off < kWave; off *= 2) {
+    const int below = __shfl_up(v, off);
+    if (lane >= off) v += below;
+  }
+  return v;
+}
+
+// The counts of a digit over the tiles become the words of that digit before each
+// tile.
+__global__ __launch_bounds__(kBlock) void k_embed_scan(SortPass p, int32_t* hist, int32_t* totals,
+                                                       Clear clear) {
+  const int blocks = p.digits / kTileWaves;
+  if ((int)blockIdx.x >= blocks) {
+    clear_rows(clear, (int)blockIdx.x - blocks);
+    return;
+  }
+  constexpr int kEach = 8;  // tiles of a lane at a time
+  const int lane = threadIdx.x & 63, d = (int)blockIdx.x * kTileWaves + (threadIdx.x >> 6);
+  int32_t* row = hist + (int64_t)d * p.tiles;
+  int carry = 0;
+  for (int64_t t0 = 0; t0 < p.tiles; t0 += kWave * kEach) {
+    int v[kEach], own = 0;
+#pragma unroll
+    for (int u = 0; u < kEach; u++) {
+      const int64_t t = t0 + lane * kEach + u;
+      v[u] = t < p.tiles ? row[t] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kEach; u++) own += v[u];
+    const int upto = wave_prefix(own, lane);
+    int at = carry + upto - own;
+#pragma unroll
+    for (int u = 0; u < kEach; u++) {
+      const int64_t t = t0 + lane * kEach + u;
+      if (t < p.tiles) row[t] = at;
+      at += v[u];
+    }
+    carry += __shfl(upto, kWave - 1);
+  }
+  if (lane == 0) totals[d] = carry;
+}
+
+__global__ __launch_bounds__(kBlock) void k_embed_scatter(SortPass p, const int32_t* hist,
+                                                          const int32_t* totals, uint32_t* keys,
+                                                          int32_t* at, Clear clear) {
+  if ((int)blockIdx.x >= p.tiles) {
+    clear_rows(clear, (int)blockIdx.x - p.tiles);
+    return;
+  }
+  __shared__ int s_next[kTileWaves][kDigits];  // a wavefront's next place of a digit
+  __shared__ int s_total[kTileWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int d = threadIdx.x; d < p.digits; d += kBlock)
+    for (int w = 0; w < kTileWaves; w++) s_next[w][d] = 0;
+  // a wavefront's words are consecutive
+  const int64_t first = (int64_t)blockIdx.x * kTile + wave * (kTileGroups * kWave) + lane;
+  uint32_t key[kTileGroups];
+  int32_t from[kTileGroups];
+#pragma unroll
+  for (int g = 0; g < kTileGroups; g++) {
+    const int64_t i = first + g * kWave;
+    key[g] = i < p.n ? p.key(i) : 0;
+    from[g] = i < p.n ? (p.ids != nullptr ? (int32_t)i : p.at[i]) : 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int g = 0; g < kTileGroups; g++)
+    if (first + g * kWave < p.n) atomicAdd(&s_next[wave][p.digit(key[g])], 1);
+  // the words of smaller digits, for digits that are consecutive over the threads
+  const int each = p.digits / kBlock < 1 ? 1 : p.digits / kBlock;
+  const int d0 = (int)threadIdx.x * each;
+  int own = 0;
+  for (int j = 0; j < each; j++) own += d0 + j < p.digits ? totals[d0 + j] : 0;
+  const int upto = wave_prefix(own, lane);
+  if (lane == kWave - 1) s_total[wave] = upto;
+  __syncthreads();
+  int base = upto - own;
+  for (int w = 0; w < wave; w++) base += s_total[w];
+  for (int j = 0; j < each && d0 + j < p.digits; j++) {
+    const int d = d0 + j;
+    int place = base + hist[(int64_t)d * p.tiles + blockIdx.x];
+    base += totals[d];
+#pragma unroll
+    for (int w = 0; w < kTileWaves; w++) {
+      const int count = s_next[w][d];
+      s_next[w][d] = place;
+      place += count;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int g = 0; g < kTileGroups; g++) {
+    const bool there = first + g * kWave < p.n;
+    const int d = p.digit(key[g]);
+    uint64_t set[kDigitBits];
+#pragma unroll
+    for (int b = 0; b < kDigitBits; b++) set[b] = __ballot((d >> b) & 1);
+    const uint64_t same = lanes_with(set, d) & __ballot(there);
+    const int rank = __popcll(same & lanes_below(lane));
+    const int place = s_next[wave][d] + rank;
+    // places lie in [0, n) by construction; the test keeps a fault out of reach
+    // should the tables ever disagree
+    if (there && place >= 0 && place < p.n) {
+      keys[place] = key[g];
+      at[place] = from[g];
+    }
+    // the wavefront's own counters: its reads are before its writes
+    __builtin_amdgcn_wave_barrier();
+    if (there && rank == __popcll(same) - 1) s_next[wave][d] = place + 1;
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -323,32 +536,34 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedBackwardArgs a, Colu
   Pack<float, kE> sum{};
   uint32_t word = (uint32_t)__builtin_amdgcn_readfirstlane((int)key);
   bool came = word == before;
-  for (int j0 = 0; j0 < used; j0 += kAhead) {
+  // `next`'s row comes after `word`'s
+  const auto add = [&](const Pack<TI, kE>& in, uint32_t next) {
+    if (next != word) {
+      if (came) {
+        if (l.there) put<SHORT>(head + k * cols.ld + l.first, l.left, sum);
+      } else {
+        write_word<SHORT, TG>(a, word, l, sum);
+      }
+      word = next;
+      came = false;
+      sum = Pack<float, kE>{};
+    }
+#pragma unroll
+    for (int e = 0; e < kE; e++) sum.v[e] += to_f32(in.v[e]);
+  };
+  const auto row_of = [&](int j) { return dy + __builtin_amdgcn_readlane(row, j) * a.lddy; };
+  const auto key_of = [&](int j) { return (uint32_t)__builtin_amdgcn_readlane((int)key, j); };
+  int j0 = 0;
+  for (; j0 + kAhead <= used; j0 += kAhead) {
     Pack<TI, kE> in[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; u++) {
-      const int j = j0 + u < used ? j0 + u : used - 1;
-      const int32_t r = __builtin_amdgcn_readlane(row, j);
-      in[u] = get<SHORT>(dy + r * a.lddy, l.left);
-    }
+    for (int u = 0; u < kAhead; u++) in[u] = get_once<SHORT>(row_of(j0 + u), l.left);
+    // every load is under way before the first is waited for
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int u = 0; u < kAhead; u++) {
-      if (j0 + u >= used) break;
-      const uint32_t next = (uint32_t)__builtin_amdgcn_readlane((int)key, j0 + u);
-      if (next != word) {
-        if (came) {
-          if (l.there) put<SHORT>(head + k * cols.ld + l.first, l.left, sum);
-        } else {
-          write_word<SHORT, TG>(a, word, l, sum);
-        }
-        word = next;
-        came = false;
-        sum = Pack<float, kE>{};
-      }
-#pragma unroll
-      for (int e = 0; e < kE; e++) sum.v[e] += to_f32(in[u].v[e]);
-    }
+    for (int u = 0; u < kAhead; u++) add(in[u], key_of(j0 + u));
   }
+  for (; j0 < used; j0++) add(get_once<SHORT>(row_of(j0), l.left), key_of(j0));
   const bool goes = word == after;
   if (!came && !goes) {
     write_word<SHORT, TG>(a, word, l, sum);
@@ -357,69 +572,145 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedBackwardArgs a, Colu
   }
 }
 
-// Joins the partial sums of the word that goes over chunk k's end and began in
-// it: one block a chunk, most of which have none. The word's last chunk is the
-// first one behind which another word follows.
-template <typename TG, bool SHORT>
-__device__ __forceinline__ void join_word(const EmbedBackwardArgs& a, const Columns& cols,
-                                          const uint32_t* keys, int chunk, int64_t k,
-                                          const float* head, const float* tail) {
-  const int64_t begin = k * chunk, end = begin + chunk;
-  const uint32_t word = keys[end - 1];
-  if (word >= (uint32_t)a.V || keys[end] != word) return;
-  if (keys[begin] == word && begin > 0 && keys[begin - 1] == word) return;
-  __shared__ int s_last;
-  __shared__ float s_sum[kBlock / kWave][kWave][kE];
-  __syncthreads();
-  if (threadIdx.x == 0) s_last = 0x7fffffff;
-  __syncthreads();
-  // the word ends in chunk k + 1 + s_last
-  for (int64_t from = 0;; from += kBlock) {
-    const int64_t stop = (k + 2 + from + threadIdx.x) * chunk;
-    if (stop >= a.n || keys[stop] != word) atomicMin(&s_last, (int)(from + threadIdx.x));
-    __syncthreads();
-    const int found = s_last;
-    __syncthreads();
-    if (found != 0x7fffffff) break;
+// Whether the word goes over the end of chunk c no further.
+__device__ __forceinline__ bool ends_in(const uint32_t* keys, int64_t n, int chunk, int64_t c,
+                                        uint32_t word) {
+  const int64_t stop = (c + 1) * chunk;
+  return stop >= n || keys[stop] != word;
+}
+
+// The chunk in which a word that goes over chunk k's end comes to its own: by 64
+// probes at a time, first of the next chunks, then evenly over the others.
+__device__ __forceinline__ int64_t last_chunk(const uint32_t* keys, int64_t n, int chunk,
+                                              int64_t k, uint32_t word) {
+  const int lane = threadIdx.x & 63;
+  int64_t low = k + 1, high = (n - 1) / chunk, step = 1;
+  for (;;) {
+    const int64_t c = low + lane * step < high ? low + lane * step : high;
+    const uint64_t m = __ballot(ends_in(keys, n, chunk, c, word));
+    if (m == 0) {
+      low += 63 * step + 1;
+    } else {
+      const int f = __builtin_ctzll(m);
+      const int64_t found = low + f * step < high ? low + f * step : high;
+      if (step == 1 || found == low) return found;
+      low = f > 0 ? low + (f - 1) * step + 1 : low;
+      high = found;
+    }
+    step = (high - low) / 63 > 1 ? (high - low) / 63 : 1;
   }
-  constexpr int kWaves = kBlock / kWave;
-  const int count = s_last + 1;
-  const LaneColumns l = lane_columns<SHORT>(cols, a.D);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const float* from = head + (k + 1) * cols.ld + l.first;
-  Pack<float, kE> sum{};
-  for (int j0 = wave; j0 < count; j0 += kAhead * kWaves) {
+}
+
+// Rows [first, first + count), every `stride`-th, of a table of partial sums.
+template <bool SHORT>
+__device__ __forceinline__ void add_rows(const float* rows, int64_t ld, int count, int first,
+                                         int stride, int left, Pack<float, kE>& sum) {
+  for (int j0 = first; j0 < count; j0 += kAhead * stride) {
     Pack<float, kE> in[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; u++) {
-      const int j = j0 + u * kWaves;
-      in[u] = get<SHORT>(from + (j < count ? j : j0) * cols.ld, l.left);
+      const int j = j0 + u * stride;
+      in[u] = get<SHORT>(rows + (j < count ? j : j0) * ld, left);
     }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int u = 0; u < kAhead; u++) {
-      if (j0 + u * kWaves >= count) break;
+    for (int u = 0; u < kAhead; u++)
 #pragma unroll
-      for (int e = 0; e < kE; e++) sum.v[e] += in[u].v[e];
-    }
+      for (int e = 0; e < kE; e++) sum.v[e] += j0 + u * stride < count ? in[u].v[e] : 0.0f;
   }
+}
+
+// Long words' partial sums, kSpan chunks to one: for each span of chunks that lies
+// wholly within a word that comes into it.
+constexpr int kSpan = 32;
+constexpr int kWaves = kBlock / kWave;
+
+// The waves' sums, in their order, to wave 0.
+__device__ __forceinline__ void join_waves(float (&s_sum)[kWaves][kWave][kE],
+                                           Pack<float, kE>& sum) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int e = 0; e < kE; e++) s_sum[wave][lane][e] = sum.v[e];
   __syncthreads();
   if (wave != 0) return;
-  sum = get<SHORT>(tail + k * cols.ld + l.first, l.left);
 #pragma unroll
-  for (int w = 0; w < kWaves; w++)
+  for (int w = 1; w < kWaves; w++)
 #pragma unroll
     for (int e = 0; e < kE; e++) sum.v[e] += s_sum[w][lane][e];
-  write_word<SHORT, TG>(a, word, l, sum);
 }
 
+template <bool SHORT>
+__global__ __launch_bounds__(kBlock) void k_embed_spans(EmbedBackwardArgs a, Columns cols,
+                                                        const uint32_t* keys, int chunk,
+                                                        const float* head, float* spans) {
+  __shared__ float s_sum[kWaves][kWave][kE];
+  const int64_t first = (int64_t)blockIdx.x * kSpan * chunk, last = first + kSpan * chunk - 1;
+  if (first == 0 || last >= a.n) return;
+  const uint32_t word = keys[first];
+  if (word >= (uint32_t)a.V || keys[first - 1] != word || keys[last] != word) return;
+  const LaneColumns l = lane_columns<SHORT>(cols, a.D);
+  Pack<float, kE> sum{};
+  add_rows<SHORT>(head + (int64_t)blockIdx.x * kSpan * cols.ld + l.first, cols.ld, kSpan,
+                  threadIdx.x >> 6, kWaves, l.left, sum);
+  join_waves(s_sum, sum);
+  if (threadIdx.x < kWave && l.there) put<SHORT>(spans + blockIdx.x * cols.ld + l.first, l.left, sum);
+}
+
+// Joins the partial sums of the words that go over their chunk's end and began in
+// it: a wavefront a chunk, most of which have none, but all four of a block for
+// words over many chunks. In order: the word's own tail, the chunks up to a span,
+// the spans, the chunks behind.
 template <typename TG, bool SHORT>
 __global__ __launch_bounds__(kBlock) void k_embed_join(EmbedBackwardArgs a, Columns cols,
                                                        const uint32_t* keys, int chunk,
-                                                       const float* head, const float* tail) {
-  for (int64_t k = blockIdx.x; (k + 1) * chunk < a.n; k += gridDim.x)
-    join_word<TG, SHORT>(a, cols, keys, chunk, k, head, tail);
+                                                       int64_t chunks, const float* head,
+                                                       const float* tail, const float* spans) {
+  constexpr int kAlone = 2 * kAhead;
+  __shared__ float s_sum[kWaves][kWave][kE];
+  __shared__ int s_count[kWaves];  // chunks that the word of each wave's chunk goes on for
+  const int wave = threadIdx.x >> 6;
+  const LaneColumns l = lane_columns<SHORT>(cols, a.D);
+  for (int64_t k0 = (int64_t)blockIdx.x * kWaves; k0 + 1 < chunks; k0 += (int64_t)gridDim.x * kWaves) {
+    const int64_t k = k0 + wave, begin = k * chunk, end = begin + chunk;
+    uint32_t word = (uint32_t)a.V;
+    if (k + 1 < chunks) {
+      word = keys[end - 1];
+      const bool goes = word < (uint32_t)a.V && keys[end] == word;
+      const bool came = keys[begin] == word && begin > 0 && keys[begin - 1] == word;
+      if (!goes || came) word = (uint32_t)a.V;
+    }
+    int count = 0;
+    if (word < (uint32_t)a.V) count = (int)(last_chunk(keys, a.n, chunk, k, word) - k);
+    if (count > 0 && count <= kAlone) {
+      Pack<float, kE> sum = get<SHORT>(tail + k * cols.ld + l.first, l.left);
+      add_rows<SHORT>(head + (k + 1) * cols.ld + l.first, cols.ld, count, 0, 1, l.left, sum);
+      write_word<SHORT, TG>(a, word, l, sum);
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s_count[wave] = count;
+    __syncthreads();
+    for (int w = 0; w < kWaves; w++) {
+      const int all = s_count[w];
+      if (all <= kAlone) continue;
+      const int64_t own = k0 + w, from = own + 1, to = from + all;
+      // a span with the word's last chunk, which it may not fill, has no sum
+      int64_t g0 = (from + kSpan - 1) / kSpan, g1 = (to - 1) / kSpan;
+      if (spans == nullptr || g1 <= g0) g0 = g1 = to / kSpan + 1;
+      const int64_t stop = g0 * kSpan < to ? g0 * kSpan : to, on = g1 * kSpan < to ? g1 * kSpan : to;
+      Pack<float, kE> sum{};
+      if (wave == 0) sum = get<SHORT>(tail + own * cols.ld + l.first, l.left);
+      add_rows<SHORT>(head + from * cols.ld + l.first, cols.ld, (int)(stop - from), wave, kWaves,
+                      l.left, sum);
+      if (g1 > g0)
+        add_rows<SHORT>(spans + g0 * cols.ld + l.first, cols.ld, (int)(g1 - g0), wave, kWaves,
+                        l.left, sum);
+      add_rows<SHORT>(head + on * cols.ld + l.first, cols.ld, (int)(to - on), wave, kWaves, l.left,
+                      sum);
+      join_waves(s_sum, sum);
+      if (wave == 0) write_word<SHORT, TG>(a, keys[own * chunk + chunk - 1], l, sum);
+      __syncthreads();
+    }
+  }
 }
 
 Columns columns_of(int32_t D) {
@@ -448,13 +739,15 @@ size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 struct Workspace {
   uint32_t *keys, *sorted;
-  int32_t* at;
-  float *head, *tail;
-  void* temp;
+  int32_t *at, *at_before, *hist, *totals;
+  uint8_t* taken;
+  float *head, *tail, *spans;
   size_t bytes;
 };
 
-Workspace lay_out(void* base, int32_t n, int32_t D) {
+int64_t tiles_of(int32_t n) { return ((int64_t)n + kTile - 1) / kTile; }
+
+Workspace lay_out(void* base, int32_t n, int32_t V, int32_t D) {
   Workspace w{};
   size_t used = 0;
   const auto take = [&](size_t bytes) {
@@ -465,15 +758,85 @@ Workspace lay_out(void* base, int32_t n, int32_t D) {
   const int64_t chunks = ((int64_t)n + chunk_of(n) - 1) / chunk_of(n);
   w.sorted = (uint32_t*)take(4 * (size_t)n);
   w.at = (int32_t*)take(4 * (size_t)n);
-  const size_t partial = 4 * (size_t)chunks * (size_t)columns_of(D).ld;
-  w.head = (float*)take(partial);
-  w.tail = (float*)take(partial);
+  const size_t row = 4 * (size_t)columns_of(D).ld;
+  w.head = (float*)take((size_t)chunks * row);
+  w.tail = (float*)take((size_t)chunks * row);
+  w.spans = (float*)take((size_t)(chunks / kSpan) * row);
   if (n > kSortMax) {
     w.keys = (uint32_t*)take(4 * (size_t)n);
-    w.temp = take(radix_sort_temp_bytes(n, 4));
+    w.at_before = (int32_t*)take(4 * (size_t)n);
+    w.hist = (int32_t*)take(4 * (size_t)tiles_of(n) * kDigits);
+    w.totals = (int32_t*)take(4 * kDigits);
+    w.taken = (uint8_t*)take(((size_t)V + 511) / 512 * 512);
   }
   w.bytes = used;
   return w;
+}
+
+template <int GROUPS>
+void launch_sort(const EmbedBackwardArgs& a, const Workspace& w, const Clear& clear, int bits,
+                 hipStream_t s) {
+  hipLaunchKernelGGL(k_embed_sort<GROUPS>, dim3(1 + clear.blocks), dim3(kSortWaves * kWave), 0, s,
+                     a.ids, a.n, a.V, bits, w.sorted, w.at, a.status, clear);
+}
+
+// Sorts the positions by word into w.sorted and w.at, and clears the gradient.
+void launch_order(const EmbedBackwardArgs& a, const Workspace& w, hipStream_t s) {
+  const int bits = key_bits(a.V);
+  if (a.n <= kSortMax) {
+    const Clear clear = clear_of(a, 0, a.V, kSortWaves * kWave);
+    const int groups = (a.n + kSortWaves * kWave - 1) / (kSortWaves * kWave);
+    if (groups <= 1) return launch_sort<1>(a, w, clear, bits, s);
+    if (groups <= 2) return launch_sort<2>(a, w, clear, bits, s);
+    if (groups <= 4) return launch_sort<4>(a, w, clear, bits, s);
+    return launch_sort<8>(a, w, clear, bits, s);
+  }
+  const int passes = (bits + kDigitBits - 1) / kDigitBits;
+  const int digit_bits = (bits + passes - 1) / passes < 2 ? 2 : (bits + passes - 1) / passes;
+  SortPass p{};
+  p.n = a.n;
+  p.V = a.V;
+  p.digits = 1 << digit_bits;
+  p.tiles = (int32_t)tiles_of(a.n);
+  p.status = a.status;
+  p.ids = a.ids;
+  const int launches = 3 * passes - 1;  // that clear: all behind the first
+  int launch = 0;
+  const auto clear_next = [&]() {
+    const int64_t first = (int64_t)a.V * launch / launches;
+    launch++;
+    return clear_of(a, first, (int64_t)a.V * launch / launches, kBlock, w.taken);
+  };
+  if (!a.accumulate) {
+    p.taken = w.taken;
+    // the marks, as a row of bytes of their own
+    EmbedBackwardArgs marks{};
+    marks.grad = w.taken;
+    marks.grad_dtype = W2V_DTYPE_BF16;
+    marks.V = (int32_t)(((int64_t)a.V + 511) / 512);
+    marks.D = marks.ldg = 256;
+    const Clear c = clear_of(marks, 0, marks.V);
+    hipLaunchKernelGGL(k_embed_clear, dim3(c.blocks), dim3(kBlock), 0, s, c);
+  }
+  for (int pass = 0; pass < passes; pass++) {
+    p.shift = pass * digit_bits;
+    // the last pass writes the result
+    const bool to_out = (passes - 1 - pass) % 2 == 0;
+    uint32_t* keys = to_out ? w.sorted : w.keys;
+    int32_t* at = to_out ? w.at : w.at_before;
+    Clear c = pass == 0 ? Clear{} : clear_next();
+    hipLaunchKernelGGL(k_embed_count, dim3(p.tiles + c.blocks), dim3(kBlock), 0, s, p, w.hist, c);
+    c = clear_next();
+    hipLaunchKernelGGL(k_embed_scan, dim3(p.digits / kTileWaves + c.blocks), dim3(kBlock), 0, s,
+                       p, w.hist, w.totals, c);
+    c = clear_next();
+    hipLaunchKernelGGL(k_embed_scatter, dim3(p.tiles + c.blocks), dim3(kBlock), 0, s, p, w.hist,
+                       w.totals, keys, at, c);
+    p.ids = nullptr;
+    p.taken = nullptr;
+    p.keys = keys;
+    p.at = at;
+  }
 }
 
 template <typename TI, typename TG, bool SHORT>
@@ -481,13 +844,19 @@ hipError_t launch_sums(const EmbedBackwardArgs& a, const Workspace& w, hipStream
   const Columns cols = columns_of(a.D);
   const int chunk = chunk_of(a.n);
   const int64_t chunks = ((int64_t)a.n + chunk - 1) / chunk;
-  const dim3 grid((unsigned)((chunks + 3) / 4), (unsigned)cols.tiles);
-  hipLaunchKernelGGL((k_embed_sums<TI, TG, SHORT>), grid, dim3(kBlock), 0, s, a, cols, w.sorted,
-                     w.at, chunk, w.head, w.tail);
-  const int64_t joins = chunks - 1 < kMaxGrid ? chunks - 1 : kMaxGrid;
-  if (joins > 0)
-    hipLaunchKernelGGL((k_embed_join<TG, SHORT>), dim3((unsigned)joins, (unsigned)cols.tiles),
-                       dim3(kBlock), 0, s, a, cols, w.sorted, chunk, w.head, w.tail);
+  const unsigned tiles = (unsigned)cols.tiles;
+  hipLaunchKernelGGL((k_embed_sums<TI, TG, SHORT>), dim3((unsigned)((chunks + 3) / 4), tiles),
+                     dim3(kBlock), 0, s, a, cols, w.sorted, w.at, chunk, w.head, w.tail);
+  if (chunks == 1) return hipGetLastError();
+  // spans shorten words over hundreds of chunks, for a launch
+  const float* spans = chunks >= 64 * kSpan ? w.spans : nullptr;
+  if (spans != nullptr)
+    hipLaunchKernelGGL(k_embed_spans<SHORT>, dim3((unsigned)(chunks / kSpan), tiles), dim3(kBlock),
+                       0, s, a, cols, w.sorted, chunk, w.head, w.spans);
+  const int64_t joins = (chunks - 1 + kWaves - 1) / kWaves;
+  hipLaunchKernelGGL((k_embed_join<TG, SHORT>),
+                     dim3((unsigned)(joins < kMaxGrid ? joins : kMaxGrid), tiles), dim3(kBlock), 0,
+                     s, a, cols, w.sorted, chunk, chunks, w.head, w.tail, spans);
   return hipGetLastError();
 }
 
@@ -498,30 +867,14 @@ hipError_t launch_sums(const EmbedBackwardArgs& a, const Workspace& w, hipStream
 
 template <typename TG>
 hipError_t launch_backward(const EmbedBackwardArgs& a, void* workspace, hipStream_t s) {
-  const RowPacks p = row_packs(a.V, a.D);
-  const int clear = a.accumulate ? 0 : row_blocks(p);
   if (a.n == 0) {
-    if (clear > 0)
-      hipLaunchKernelGGL(k_embed_clear<TG>, dim3(clear), dim3(kBlock), 0, s, (TG*)a.grad, a.ldg,
-                         p);
+    const Clear clear = clear_of(a, 0, a.V);
+    if (clear.blocks > 0)
+      hipLaunchKernelGGL(k_embed_clear, dim3(clear.blocks), dim3(kBlock), 0, s, clear);
     return hipGetLastError();
   }
-  const Workspace w = lay_out(workspace, a.n, a.D);
-  const int bits = key_bits(a.V);
-  if (a.n <= kSortMax) {
-    // four times the threads of k_embed_clear's blocks
-    hipLaunchKernelGGL(k_embed_sort<TG>, dim3(1 + (clear + 3) / 4), dim3(kSortWaves * kWave), 0,
-                       s, a, bits, w.sorted, w.at, p);
-  } else {
-    if (clear > 0)
-      hipLaunchKernelGGL(k_embed_clear<TG>, dim3(clear), dim3(kBlock), 0, s, (TG*)a.grad, a.ldg,
-                         p);
-    hipLaunchKernelGGL(k_embed_keys, dim3((unsigned)(((int64_t)a.n + kBlock - 1) / kBlock)),
-                       dim3(kBlock), 0, s, a.ids, a.n, a.V, w.keys, a.status);
-    const hipError_t e =
-        radix_sort_pairs(w.keys, nullptr, w.sorted, w.at, a.n, bits, w.temp, s);
-    if (e != hipSuccess) return e;
-  }
+  const Workspace w = lay_out(workspace, a.n, a.V, a.D);
+  launch_order(a, w, s);
   switch (a.dtype) {
     case W2V_DTYPE_F32:
       return launch_sums<float, TG>(a, w, s);
@@ -570,7 +923,7 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t s) {
 }
 
 size_t embed_backward_workspace_bytes(int32_t n, int32_t V, int32_t D) {
-  return n == 0 ? 0 : lay_out(nullptr, n, D).bytes;
+  return n == 0 ? 0 : lay_out(nullptr, n, V, D).bytes;
 }
 
 hipError_t launch_embed_backward(const EmbedBackwardArgs& a, void* workspace, hipStream_t s) {

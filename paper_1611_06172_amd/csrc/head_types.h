@@ -51,6 +51,32 @@ __device__ __forceinline__ uint4 load_16(const void* p) {
   return v;
 }
 
+// 16-byte groups of data that is read or written once and is larger than the
+// caches: with a hint that keeps it from driving out what is used again.
+typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+typedef uint32_t word4_anywhere __attribute__((ext_vector_type(4), aligned(1)));
+
+template <typename P>
+__device__ __forceinline__ P load_once(const void* p) {
+  static_assert(sizeof(P) % 16 == 0, "whole groups");
+  word4 w[sizeof(P) / 16];
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(P) / 16); i++)
+    w[i] = __builtin_nontemporal_load((const word4_anywhere*)p + i);
+  P out;
+  __builtin_memcpy(&out, w, sizeof(P));
+  return out;
+}
+template <typename P>
+__device__ __forceinline__ void store_once(void* p, const P& v) {
+  static_assert(sizeof(P) % 16 == 0, "whole groups");
+  word4 w[sizeof(P) / 16];
+  __builtin_memcpy(w, &v, sizeof(P));
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(P) / 16); i++)
+    __builtin_nontemporal_store(w[i], (word4_anywhere*)p + i);
+}
+
 // The elements of 16 bytes, taken from whole words: the pack stays in four
 // registers.
 template <typename T>
