@@ -159,51 +159,80 @@ __device__ __forceinline__ void store_as(void* y, int64_t at, float v) {
 // x in LDS as the instruction wants it, for `blocks` blocks of columns at a time:
 // [block][tile of rows][piece][lane] of 16 bytes, and behind these -24 sum(x) of
 // each group and row.
-template <typename T, int MT, int GB>
+// A wavefront takes kUnits groups of 16 rows at a time, whose loads are on their way
+// together (one between products, where the registers are taken); only the end of a
+// row is loaded with a test.
+template <typename T, int MT, int GB, int WAVES, bool ONCE>
 __device__ __forceinline__ void stage(const LinearQ4Args& a, const Q4Shape& q, int m0, int b0,
                                       int blocks, uint4* frags, float* sums) {
   typedef Operand<T> Op;
+  constexpr int kUnits = ONCE ? 4 / GB : 1;
   const int lane = threadIdx.x & 63, r = lane & 15, quad = lane >> 4;
-  for (int u = threadIdx.x >> 6; u < blocks / GB * MT; u += kWaves) {
-    const int g = u / MT, mt = u % MT, m = m0 + mt * 16 + r;
-    float sum = 0.0f;
+  const int units = blocks / GB * MT;
+  const T* x = (const T*)a.x;
+  for (int u0 = threadIdx.x >> 6; u0 < units; u0 += WAVES * kUnits) {
+    Pack<T, 8> in[kUnits][GB];
+    int64_t from[kUnits][GB];
+    int there[kUnits][GB];
 #pragma unroll
-    for (int b = 0; b < GB; b++) {
-      const int block = g * GB + b;
-      const int64_t k = ((int64_t)b0 + block) * 32 + quad * 8;
-      Pack<T, 8> in;
+    for (int i = 0; i < kUnits; i++) {
+      const int u = u0 + i * WAVES, g = u / MT, m = m0 + u % MT * 16 + r;
 #pragma unroll
-      for (int j = 0; j < 8; j++) in.v[j] = T(0.0f);
-      if (m < a.M && k < q.K) in = load_some<T, 8>((const T*)a.x + m * a.ldx + k, q.K - k);
-      uint4* to = frags + ((block * MT + mt) * Op::kPieces) * kWave + lane;
-      if constexpr (Op::kPieces == 1) {
-        to[0] = __builtin_bit_cast(uint4, in);
-#pragma unroll
-        for (int j = 0; j < 8; j++) sum += to_f32(in.v[j]);
-      } else {
-        uint32_t piece[3][8];
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-          float v = in.v[j];
-          sum += v;
-#pragma unroll
-          for (int p = 0; p < 3; p++) {
-            piece[p][j] = upper(v);
-            v -= __builtin_bit_cast(float, piece[p][j] << 16);
-          }
-        }
-#pragma unroll
-        for (int p = 0; p < 3; p++) {
-          uint32_t w[4];
-#pragma unroll
-          for (int j = 0; j < 4; j++) w[j] = piece[p][2 * j] | piece[p][2 * j + 1] << 16;
-          to[p * kWave] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+      for (int b = 0; b < GB; b++) {
+        const int64_t k = ((int64_t)b0 + g * GB + b) * 32 + quad * 8;
+        const bool some = u < units && m < a.M && k < q.K;
+        there[i][b] = !some ? 0 : q.K - k < 8 ? (int)(q.K - k) : 8;
+        from[i][b] = some ? m * a.ldx + k : 0;
+        if (q.K >= 8) in[i][b] = load_pack<T, 8>(x + (there[i][b] == 8 ? from[i][b] : 0));
       }
     }
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if (quad == 0) sums[(g * MT + mt) * 16 + r] = -24.0f * sum;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < kUnits; i++) {
+      const int u = u0 + i * WAVES, g = u / MT, mt = u % MT;
+      if (u >= units) break;
+      float sum = 0.0f;
+#pragma unroll
+      for (int b = 0; b < GB; b++) {
+        Pack<T, 8> v = in[i][b];
+        if (there[i][b] < 8) {
+          if (there[i][b] > 0) {
+            v = load_some<T, 8>(x + from[i][b], there[i][b]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; j++) v.v[j] = T(0.0f);
+          }
+        }
+        uint4* to = frags + (((g * GB + b) * MT + mt) * Op::kPieces) * kWave + lane;
+        if constexpr (Op::kPieces == 1) {
+          to[0] = __builtin_bit_cast(uint4, v);
+#pragma unroll
+          for (int j = 0; j < 8; j++) sum += to_f32(v.v[j]);
+        } else {
+          uint32_t piece[3][8];
+#pragma unroll
+          for (int j = 0; j < 8; j++) {
+            float left = v.v[j];
+            sum += left;
+#pragma unroll
+            for (int p = 0; p < 3; p++) {
+              piece[p][j] = upper(left);
+              left -= __builtin_bit_cast(float, piece[p][j] << 16);
+            }
+          }
+#pragma unroll
+          for (int p = 0; p < 3; p++) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; j++) w[j] = piece[p][2 * j] | piece[p][2 * j + 1] << 16;
+            to[p * kWave] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (quad == 0) sums[(g * MT + mt) * 16 + r] = -24.0f * sum;
+    }
   }
 }
 
@@ -245,152 +274,256 @@ __device__ __forceinline__ void add_group(const uint4* frags, const float* sums,
       for (int i = 0; i < 4; i++) acc[t][mt][i] = fmaf(scale[t], part[t][mt][i], acc[t][mt][i]);
 }
 
-// The blocks [b0, b0 + blocks) of NT tiles; `words` and `scales` are the first
-// tile's, `next` tiles on (0 where there is no second one).
-template <typename T, int MT, int NT, int GB>
-__device__ __forceinline__ void add_blocks(const Q4Shape& q, const uint32_t* words,
-                                           const bf16_t* scales, int next, int b0, int blocks,
-                                           const uint4* frags, const float* sums,
-                                           f32x4 (&acc)[NT][MT]) {
-  const int lane = threadIdx.x & 63, r = lane & 15;
-  const int64_t word_step = (int64_t)next * q.blocks * 64, scale_step = (int64_t)next * q.groups * 16;
-  int b = 0;
-  for (; b + 4 <= blocks; b += 4) {
-    uint4 w[NT];
-    float s[NT][4 / GB];
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
-      w[t] = load_16(words + t * word_step + (int64_t)((b0 + b) >> 2) * 256 + lane * 4);
-#pragma unroll
-      for (int g = 0; g < 4 / GB; g++)
-        s[t][g] = to_f32(scales[t * scale_step + scale_at(q.groups, (b0 + b) / GB + g, r)]);
-    }
-#pragma unroll
-    for (int g = 0; g < 4 / GB; g++) {
-      uint32_t word[NT][GB];
-      float scale[NT];
-#pragma unroll
-      for (int t = 0; t < NT; t++) {
-        const uint32_t four[4] = {w[t].x, w[t].y, w[t].z, w[t].w};
-#pragma unroll
-        for (int i = 0; i < GB; i++) word[t][i] = four[g * GB + i];
-        scale[t] = s[t][g];
-      }
-      add_group<T, MT, NT, GB>(frags, sums, b + g * GB, word, scale, acc);
-    }
-  }
-  // the rest of a row's blocks: none where a group has four
-  if constexpr (GB < 4) {
-    for (; b < blocks; b += GB) {
-      uint32_t word[NT][GB];
-      float scale[NT];
-#pragma unroll
-      for (int t = 0; t < NT; t++) {
-#pragma unroll
-        for (int i = 0; i < GB; i++)
-          word[t][i] = words[t * word_step + word_at(q.blocks, b0 + b + i, lane)];
-        scale[t] = to_f32(scales[t * scale_step + scale_at(q.groups, (b0 + b) / GB, r)]);
-      }
-      add_group<T, MT, NT, GB>(frags, sums, b, word, scale, acc);
-    }
-  }
+// Cache policy of the words, which are read once: they do not drive x and the scales
+// out (1 x 10^6 x 300: 57 to 52 us).
+constexpr int kNonTemporal = 2;
+
+// Range-checked access to `bytes` bytes: loads past them are 0.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t checked(const void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)p, (short)0, bytes, 0x00020000);
 }
 
-// One block: sets of kWaves x NT tiles of W, against MT tiles of x (blockIdx.y).
-// `span` blocks of columns are in LDS at once; where that is all of them they are
-// put there once.
-template <typename T, int MT, int NT, int GB>
-__global__ __launch_bounds__(kBlock) void k_linear_q4(LinearQ4Args a, Q4Shape q, int span) {
+// Four blocks of columns of NT tiles (the last of a row: the rest): a lane's words
+// and the scales of its row. Four scales that lie together come in one load, others
+// one by one; which it was is only looked at when they are used. What a rest's loads
+// take in of other lanes and rows is not used.
+template <int NT, int GB>
+struct Step {
+  word4 w[NT];
+  static constexpr int kSingle = 4 / GB < 3 ? 4 / GB : 3;
+  uint32_t four[NT][2];
+  uint16_t single[NT][kSingle];
+  float bias[NT];
+
+  __device__ __forceinline__ float scale(int t, int g, bool whole) const {
+    const uint32_t bits = GB == 1 && whole ? four[t][g / 2] >> (16 * (g & 1))
+                                           : single[t][g < kSingle ? g : 0];
+    return __builtin_bit_cast(float, bits << 16);
+  }
+};
+
+// Whether the scales of a step that begins with `block` lie in fours.
+template <int GB>
+__device__ __forceinline__ bool whole_scales(const Q4Shape& q, int block) {
+  return q.groups - (block / GB & ~3) >= 4;
+}
+
+// The next NT tiles of a wavefront, with what they have of words, scales and bias
+// in range: nothing for tiles that there are not.
+template <int NT, int GB>
+struct Tiles {
+  __amdgpu_buffer_rsrc_t words, scales, bias;
+
+  __device__ __forceinline__ void begin(const LinearQ4Args& a, const Q4Shape& q, int64_t tile) {
+    const int64_t left = q.tiles - tile;
+    const int count = left >= NT ? NT : left > 0 ? (int)left : 0;
+    const int64_t rows = q.N - tile * 16;
+    words = checked(a.packed + tile * q.blocks * 64, count * q.blocks * 256);
+    scales = checked((const bf16_t*)a.scales + tile * q.groups * 16, count * q.groups * 32);
+    bias = checked(a.bias + tile * 16,
+                   a.bias == nullptr || rows <= 0 ? 0 : (rows < NT * 16 ? (int)rows : NT * 16) * 4);
+  }
+  __device__ __forceinline__ void load(const Q4Shape& q, int block, Step<NT, GB>& step) const {
+    const int lane = threadIdx.x & 63, r = lane & 15;
+    const int rest = q.blocks - block;
+    const int group = block / GB, first = group & ~3;
+    const bool whole = whole_scales<GB>(q, block);
+    step = Step<NT, GB>{};  // nothing of the step before is kept alive
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+      const int from = (t * q.blocks + block) * 256;
+      if (rest >= 4) {
+        step.w[t] = __builtin_amdgcn_raw_buffer_load_b128(words, lane * 16, from, kNonTemporal);
+      } else {
+        const int at = lane * rest * 4;
+        step.w[t].x = __builtin_amdgcn_raw_buffer_load_b32(words, at, from, 0);
+        step.w[t].y = __builtin_amdgcn_raw_buffer_load_b32(words, at + 4, from, 0);
+        step.w[t].z = __builtin_amdgcn_raw_buffer_load_b32(words, at + 8, from, 0);
+      }
+      const int row = t * q.groups * 32 + first * 32 + (group - first) * 2;
+      if (GB == 1 && whole) {
+        const auto four = __builtin_amdgcn_raw_buffer_load_b64(scales, r * 8, row, 0);
+        step.four[t][0] = four[0];
+        step.four[t][1] = four[1];
+      } else {
+        const int at = whole ? r * 8 : r * (q.groups - first) * 2;
+#pragma unroll
+        for (int g = 0; g < Step<NT, GB>::kSingle; g++)
+          step.single[t][g] = __builtin_amdgcn_raw_buffer_load_b16(scales, at + 2 * g, row, 0);
+      }
+      // in time for the step that ends the tile; with larger groups a test costs more
+      // than the load (61 x 100,000 x 600 in groups of 64: 31 to 29 us)
+      if (GB > 1 || rest <= 4)
+        step.bias[t] = __builtin_bit_cast(
+            float, __builtin_amdgcn_raw_buffer_load_b32(bias, r * 4, t * 64, 0));
+    }
+  }
+};
+
+// Wavefronts of a SIMD that the registers are to allow.
+constexpr int resident_waves(int mt) { return mt == 1 ? 4 : mt == 2 ? 3 : 2; }
+
+// One block: sets of WAVES x NT tiles of W, against MT tiles of x (blockIdx.y).
+// `span` blocks of columns of x are in LDS at once; where that is all of them (ONCE)
+// they are put there once. A wavefront goes through its steps of all sets with the next
+// one's loads on their way.
+template <typename T, int MT, int NT, int GB, int WAVES, bool ONCE>
+__global__ __launch_bounds__(WAVES* kWave, resident_waves(MT)) void k_linear_q4(LinearQ4Args a, Q4Shape q, int span) {
   extern __shared__ uint4 frags[];
   float* sums = (float*)(frags + (int64_t)span * MT * Operand<T>::kPieces * kWave);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15;
+  const int lane = threadIdx.x & 63, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m0 = blockIdx.y * MT * 16;
-  const bool once = span >= q.blocks;
-  if (once) {
-    stage<T, MT, GB>(a, q, m0, 0, q.blocks, frags, sums);
-    __syncthreads();
-  }
-  const int64_t sets = (q.tiles + kWaves * NT - 1) / (kWaves * NT);
-  for (int64_t set = blockIdx.x; set < sets; set += gridDim.x) {
-    const int64_t tile = (set * kWaves + wave) * NT;
-    const bool any = tile < q.tiles;
-    const uint32_t* words = a.packed + (any ? tile : 0) * q.blocks * 64;
-    const bf16_t* scales = (const bf16_t*)a.scales + (any ? tile : 0) * q.groups * 16;
-    const int next = tile + 1 < q.tiles ? 1 : 0;
-    f32x4 acc[NT][MT] = {};
-    if (once) {
-      if (any)
-        add_blocks<T, MT, NT, GB>(q, words, scales, next, 0, q.blocks, frags, sums, acc);
-    } else {
-      for (int b0 = 0; b0 < q.blocks; b0 += span) {
-        const int blocks = q.blocks - b0 < span ? q.blocks - b0 : span;
-        __syncthreads();
-        stage<T, MT, GB>(a, q, m0, b0, blocks, frags, sums);
-        __syncthreads();
-        if (any) add_blocks<T, MT, NT, GB>(q, words, scales, next, b0, blocks, frags, sums, acc);
-      }
+  const int64_t sets = (q.tiles + WAVES * NT - 1) / (WAVES * NT);
+  f32x4 acc[NT][MT] = {};
+  // where the loads and the products are
+  int64_t load_set = blockIdx.x, set = blockIdx.x;
+  int load_block = 0, block = 0;
+  Tiles<NT, GB> tiles;
+  tiles.begin(a, q, (load_set * WAVES + wave) * NT);
+  const auto load = [&](Step<NT, GB>& step) {
+    tiles.load(q, load_block, step);
+    load_block += 4;
+    if (load_block >= q.blocks) {
+      load_block = 0;
+      load_set += gridDim.x;
+      tiles.begin(a, q, (load_set * WAVES + wave) * NT);
     }
+  };
+  const auto add = [&](const Step<NT, GB>& step) {
+    const int staged = ONCE ? block : block % span;
+    if (!ONCE && staged == 0) {
+      __syncthreads();
+      stage<T, MT, GB, WAVES, false>(a, q, m0, block, q.blocks - block < span ? q.blocks - block : span,
+                                     frags, sums);
+      __syncthreads();
+    }
+    const bool whole = whole_scales<GB>(q, block);
+#pragma unroll
+    for (int g = 0; g < 4 / GB; g++) {
+      if (block + g * GB >= q.blocks) break;
+      uint32_t word[NT][GB];
+      float scale[NT];
+#pragma unroll
+      for (int t = 0; t < NT; t++) {
+#pragma unroll
+        for (int i = 0; i < GB; i++) word[t][i] = step.w[t][g * GB + i];
+        scale[t] = step.scale(t, g, whole);
+      }
+      add_group<T, MT, NT, GB>(frags, sums, staged + g * GB, word, scale, acc);
+    }
+    block += 4;
+    if (block < q.blocks) return;
+    const int64_t tile = (set * WAVES + wave) * NT;
 #pragma unroll
     for (int t = 0; t < NT; t++) {
       const int64_t n = (tile + t) * 16 + r;
-      if (n >= q.N) continue;
-      const float bias = a.bias != nullptr ? a.bias[n] : 0.0f;
+      if (n < q.N) {
 #pragma unroll
-      for (int mt = 0; mt < MT; mt++)
+        for (int mt = 0; mt < MT; mt++)
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const int m = m0 + mt * 16 + (lane >> 4) * 4 + i;
-          if (m >= a.M) continue;
-          const int64_t at = m * a.ldy + n;
-          const float v = acc[t][mt][i] + bias;
-          if (a.out_dtype == W2V_DTYPE_F32) {
-            store_as<float>(a.y, at, v);
-          } else {
-            store_as<typename Operand<T>::Element>(a.y, at, v);
+          for (int i = 0; i < 4; i++) {
+            const int m = m0 + mt * 16 + (lane >> 4) * 4 + i;
+            if (m >= a.M) continue;
+            const int64_t at = m * a.ldy + n;
+            const float v = acc[t][mt][i] + step.bias[t];
+            if (a.out_dtype == W2V_DTYPE_F32) {
+              store_as<float>(a.y, at, v);
+            } else {
+              store_as<typename Operand<T>::Element>(a.y, at, v);
+            }
           }
-        }
+      }
+#pragma unroll
+      for (int mt = 0; mt < MT; mt++) acc[t][mt] = f32x4{};
     }
+    block = 0;
+    set += gridDim.x;
+  };
+  Step<NT, GB> even, odd;
+  load(even);
+  if (ONCE) {
+    stage<T, MT, GB, WAVES, true>(a, q, m0, 0, q.blocks, frags, sums);
+    __syncthreads();
+  }
+  while (set < sets) {
+    load(odd);
+    add(even);
+    if (set >= sets) break;
+    load(even);
+    add(odd);
   }
 }
 
-constexpr int kMostLds = 128 << 10;
+constexpr int kMostLds = 128 << 10, kLds = 160 << 10;
 
-template <typename T, int MT, int NT, int GB>
-hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
-  constexpr int kBlockBytes = MT * Operand<T>::kPieces * kWave * 16 + MT * 16 * 4 / GB;
-  const int most = kMostLds / kBlockBytes & ~3;
-  const int span = q.blocks < most ? q.blocks : most;
-  const int bytes = span * kBlockBytes + 64;
-  const int64_t sets = (q.tiles + kWaves * NT - 1) / (kWaves * NT);
-  // as many blocks as the card holds at once: each puts x into LDS for itself
-  const int64_t held = (160 << 10) / bytes, fit = 256 * (held < 6 ? held : 6);
+// LDS of a block of columns of x.
+template <typename T>
+constexpr int block_bytes(int mt, int gb) {
+  return mt * Operand<T>::kPieces * kWave * 16 + mt * 16 * 4 / gb;
+}
+// Blocks of columns of x that LDS holds.
+template <typename T>
+int most_blocks(int mt, int group) {
+  return kMostLds / block_bytes<T>(mt, group / 32) & ~3;
+}
+
+template <typename T, int MT, int GB, int WAVES, bool ONCE>
+hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, int span, hipStream_t s) {
+  constexpr int NT = 2;
+  const int bytes = span * block_bytes<T>(MT, GB);
+  const int64_t sets = (q.tiles + WAVES * NT - 1) / (WAVES * NT);
+  // as many blocks as the card holds at once, so that all end at the same time:
+  // each puts x into LDS for itself
+  const int64_t by_lds = kLds / bytes, by_registers = resident_waves(MT) * 4 / WAVES;
+  const int64_t fit = 256 * (by_lds < by_registers ? by_lds : by_registers);
   const dim3 grid((unsigned)(sets < fit ? sets : fit), (unsigned)((a.M + MT * 16 - 1) / (MT * 16)));
   if (bytes > (64 << 10)) {
-    const hipError_t e = hipFuncSetAttribute((const void*)k_linear_q4<T, MT, NT, GB>,
+    const hipError_t e = hipFuncSetAttribute((const void*)k_linear_q4<T, MT, NT, GB, WAVES, ONCE>,
                                              hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((k_linear_q4<T, MT, NT, GB>), grid, dim3(kBlock), bytes, s, a, q, span);
+  hipLaunchKernelGGL((k_linear_q4<T, MT, NT, GB, WAVES, ONCE>), grid, dim3(WAVES * kWave), bytes,
+                     s, a, q, span);
   return hipGetLastError();
 }
 
-template <typename T, int MT, int NT>
+// Blocks of four wavefronts while LDS holds as many of them as the registers do, else
+// one block of all those wavefronts, which shares its x: of 1 x 100,000 x 1,000 fp32
+// 37 us with four of 16.
+template <typename T, int MT, int GB>
+hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
+  constexpr int kAll = resident_waves(MT) * 4;
+  const int most = most_blocks<T>(MT, GB * 32);
+  if (q.blocks > most) return launch<T, MT, GB, kAll, false>(a, q, most, s);
+  if (MT < 4 && q.blocks * block_bytes<T>(MT, GB) <= kLds / resident_waves(MT))
+    return launch<T, MT, GB, MT < 4 ? 4 : kAll, true>(a, q, q.blocks, s);
+  return launch<T, MT, GB, kAll, true>(a, q, q.blocks, s);
+}
+
+template <typename T, int MT>
 hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
   switch (q.group) {
     case 32:
-      return launch<T, MT, NT, 1>(a, q, s);
+      return launch<T, MT, 1>(a, q, s);
     case 64:
-      return launch<T, MT, NT, 2>(a, q, s);
+      return launch<T, MT, 2>(a, q, s);
     default:
-      return launch<T, MT, NT, 4>(a, q, s);
+      return launch<T, MT, 4>(a, q, s);
   }
 }
 
+// Up to 64 rows of x to a reading of W (32 of fp32, which takes three times the LDS),
+// fewer where they do not fit into LDS: reading W again costs less than x (32 x
+// 100,000 x 1,000 fp32 101 us with x in two parts).
 template <typename T>
 hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
-  if (a.M <= 16) return launch<T, 1, 2>(a, q, s);
-  if (a.M <= 32 || Operand<T>::kPieces > 1) return launch<T, 2, 2>(a, q, s);
-  return launch<T, 4, 2>(a, q, s);
+  int mt = a.M <= 16 ? 1 : a.M <= 32 || Operand<T>::kPieces > 1 ? 2 : 4;
+  while (mt > 1 && q.blocks > most_blocks<T>(mt, q.group)) mt /= 2;
+  if (mt == 1) return launch<T, 1>(a, q, s);
+  if (mt == 2) return launch<T, 2>(a, q, s);
+  if constexpr (Operand<T>::kPieces == 1) return launch<T, 4>(a, q, s);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
