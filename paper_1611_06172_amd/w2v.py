@@ -177,8 +177,11 @@ def _ptr(t) -> Optional[int]:
 
 def _stream(stream=None) -> int:
     import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    # the current stream's handle without the Stream object around it, which
+    # takes 2.5 us to make
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _dev(t, dtype, name, ndim=None):
@@ -1074,20 +1077,19 @@ def _state_rows(t, name):
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
-    if t.dim() < 1:
-        raise ValueError(f"{name} must have a first dimension")
     _here(t, name)
-    size = t.element_size()
-    rows = t.shape[0]
-    row = size
-    for n in t.shape[1:]:
+    size = t.shape
+    if len(size) < 1:
+        raise ValueError(f"{name} must have a first dimension")
+    row = t.element_size()
+    for n in size[1:]:
         row *= n
     if t.is_contiguous():
         return row, row
     if not t[0].is_contiguous():
         raise ValueError(f"{name} must have contiguous rows")
-    step = t.stride(0) * size
-    if rows > 1 and step < row:
+    step = t.stride(0) * t.element_size()
+    if size[0] > 1 and step < row:
         raise ValueError(f"{name} must have rows that do not overlap")
     return row, max(step, row)
 
@@ -1102,32 +1104,39 @@ def beam_reorder(states, parents, *, out=None, stream=None):
     states' form (not a state itself). Returns it in that form."""
     import torch
     one = isinstance(states, torch.Tensor)
-    states = [states] if one else list(states)
+    states = [states] if one else states
     _dev(parents, torch.int32, "parents", 2)
     _here(parents, "parents")
     batch, width = parents.shape
     if len(states) > MAX_BEAM_STATES:
         raise ValueError(f"at most {MAX_BEAM_STATES} states")
-    beams = 1
+    new = None if out is None else [out] if one else list(out)
+    if new is not None and len(new) != len(states):
+        raise ValueError("out must have a tensor per state")
+    beams = None
+    table = (_BeamState * max(1, len(states)))()
     with _allocations(stream):
-        if out is None:
-            new = [torch.empty((batch * width,) + tuple(t.shape[1:]), dtype=t.dtype,
-                               device=t.device) for t in states]
-        else:
-            new = [out] if one else list(out)
-            if len(new) != len(states):
-                raise ValueError("out must have a tensor per state")
-        table = (_BeamState * max(1, len(states)))()
-        for i, (t, o) in enumerate(zip(states, new)):
+        made = []
+        for i, t in enumerate(states):
             row, step = _state_rows(t, "states")
-            out_row, out_step = _state_rows(o, "out")
-            if o.dtype != t.dtype or o.shape != (batch * width,) + tuple(t.shape[1:]):
-                raise ValueError("out must have batch * width rows of the state's")
-            of = t.shape[0] // batch if batch else 1
-            if of * batch != t.shape[0] or of < 1 or (i > 0 and of != beams):
+            size = t.shape
+            of = size[0] // batch if batch else 1
+            if of * batch != size[0] or of < 1 or (beams is not None and of != beams):
                 raise ValueError("states must have batch * beams rows each")
             beams = of
-            table[i] = _BeamState(_ptr(t), step, _ptr(o), out_step, row)
-        _check(lib().w2v_beam_reorder(table, len(states), _ptr(parents), batch, beams, width,
-                                      _stream(stream)))
+            moved = (batch * width, *size[1:])
+            if new is None:
+                o, out_step = torch.empty(moved, dtype=t.dtype, device=t.device), row
+                made.append(o)
+            else:
+                o = new[i]
+                out_step = _state_rows(o, "out")[1]
+                if o.dtype != t.dtype or o.shape != moved:
+                    raise ValueError("out must have batch * width rows of the state's")
+            entry = table[i]
+            entry.src, entry.src_stride = t.data_ptr(), step
+            entry.dst, entry.dst_stride, entry.row_bytes = o.data_ptr(), out_step, row
+        _check(lib().w2v_beam_reorder(table, len(states), _ptr(parents), batch,
+                                      1 if beams is None else beams, width, _stream(stream)))
+    new = made if new is None else new
     return new[0] if one else new
