@@ -294,11 +294,11 @@ __global__ __launch_bounds__(kSortWaves* kWave) void k_embed_sort(
 
 // More words: passes over digits of up to ten bits, so that a vocabulary of up to
 // 2^20 words takes two. A block counts the digits of a tile of 2,048 words in LDS;
-// a wavefront a digit turns the tiles' counts into places; a block sends its tile
-// there in order. The gradient is cleared by further blocks of these launches,
-// which leave most of the card idle; the first one marks the rows that have words,
-// which are written later and need no zeros (10^6 words of 10^6, D 300: 17% of
-// them).
+// a block for 64 digits turns the tiles' counts into places (of few tiles, the next
+// blocks do that for themselves); a block sends its tile there in order. The gradient is cleared by further blocks of these launches,
+// which leave most of the card idle; with words for an eighth of the rows or more, the
+// first one marks the rows that have some, which are written later and need no zeros
+// (10^6 words of 10^6, D 300: 17% of them).
 constexpr int kDigitBits = 10;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kTileGroups = 8;  // of a wavefront
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_count(SortPass p, int32_t* his
     }
   __syncthreads();
   for (int d = threadIdx.x; d < p.digits; d += kBlock)
-    hist[(int64_t)d * p.tiles + blockIdx.x] = s_count[d];
+    hist[(int64_t)blockIdx.x * p.digits + d] = s_count[d];
 }
 
 __device__ __forceinline__ int wave_prefix(int v, int lane) {
@@ -353,40 +353,66 @@ __device__ __forceinline__ int wave_prefix(int v, int lane) {
   return v;
 }
 
-// The counts of a digit over the tiles become the words of that digit before each
-// tile.
-__global__ __launch_bounds__(kBlock) void k_embed_scan(SortPass p, int32_t* hist, int32_t* totals,
-                                                       Clear clear) {
-  const int blocks = p.digits / kTileWaves;
+// The counts of a digit in the tiles [tile][digit] become the words of that digit
+// before each tile: a lane a digit, a wavefront a sixteenth of up to 512 tiles at a
+// time.
+constexpr int kScanWaves = 16;
+constexpr int kScanEach = 32;
+
+__global__ __launch_bounds__(kScanWaves* kWave) void k_embed_scan(SortPass p, int32_t* hist,
+                                                                int32_t* totals, Clear clear) {
+  const int blocks = (p.digits + kWave - 1) / kWave;
   if ((int)blockIdx.x >= blocks) {
     clear_rows(clear, (int)blockIdx.x - blocks);
     return;
   }
-  constexpr int kEach = 8;  // tiles of a lane at a time
-  const int lane = threadIdx.x & 63, d = (int)blockIdx.x * kTileWaves + (threadIdx.x >> 6);
-  int32_t* row = hist + (int64_t)d * p.tiles;
+  __shared__ int s_sum[kScanWaves][kWave];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int d = (int)blockIdx.x * kWave + lane;
+  const bool there = d < p.digits;
   int carry = 0;
-  for (int64_t t0 = 0; t0 < p.tiles; t0 += kWave * kEach) {
-    int v[kEach], own = 0;
+  for (int t0 = 0; t0 < p.tiles; t0 += kScanWaves * kScanEach) {
+    const int left = p.tiles - t0 < kScanWaves * kScanEach ? p.tiles - t0 : kScanWaves * kScanEach;
+    const int each = (left + kScanWaves - 1) / kScanWaves;
+    const int first = wave * each < left ? wave * each : left;
+    const int count = left - first < each ? left - first : each;
+    int32_t* col = hist + (there ? d : 0);
+    int v[kScanEach], own = 0;
+    // no load has a test of its own
 #pragma unroll
-    for (int u = 0; u < kEach; u++) {
-      const int64_t t = t0 + lane * kEach + u;
-      v[u] = t < p.tiles ? row[t] : 0;
+    for (int u = 0; u < kScanEach; u++) {
+      const int t = t0 + first + u < p.tiles ? t0 + first + u : p.tiles - 1;
+      v[u] = col[(int64_t)t * p.digits];
     }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int u = 0; u < kEach; u++) own += v[u];
-    const int upto = wave_prefix(own, lane);
-    int at = carry + upto - own;
+    for (int u = 0; u < kScanEach; u++) {
+      v[u] = u < count ? v[u] : 0;
+      own += v[u];
+    }
+    s_sum[wave][lane] = own;
+    __syncthreads();
+    int at = carry, all = 0;
 #pragma unroll
-    for (int u = 0; u < kEach; u++) {
-      const int64_t t = t0 + lane * kEach + u;
-      if (t < p.tiles) row[t] = at;
+    for (int w = 0; w < kScanWaves; w++) {
+      at += w < wave ? s_sum[w][lane] : 0;
+      all += s_sum[w][lane];
+    }
+    carry += all;
+#pragma unroll
+    for (int u = 0; u < kScanEach; u++) {
+      if (u < count && there) col[(int64_t)(t0 + first + u) * p.digits] = at;
       at += v[u];
     }
-    carry += __shfl(upto, kWave - 1);
+    __syncthreads();
   }
-  if (lane == 0) totals[d] = carry;
+  if (wave == 0 && there) totals[d] = carry;
 }
+
+// Up to so many tiles need no launch for that (49 tiles of one pass: 50 us instead of 45
+// without it).
+constexpr int kFewTiles = 32;
 
 __global__ __launch_bounds__(kBlock) void k_embed_scatter(SortPass p, const int32_t* hist,
                                                           const int32_t* totals, uint32_t* keys,
@@ -414,20 +440,41 @@ __global__ __launch_bounds__(kBlock) void k_embed_scatter(SortPass p, const int3
 #pragma unroll
   for (int g = 0; g < kTileGroups; g++)
     if (first + g * kWave < p.n) atomicAdd(&s_next[wave][p.digit(key[g])], 1);
-  // the words of smaller digits, for digits that are consecutive over the threads
-  const int each = p.digits / kBlock < 1 ? 1 : p.digits / kBlock;
-  const int d0 = (int)threadIdx.x * each;
-  int own = 0;
-  for (int j = 0; j < each; j++) own += d0 + j < p.digits ? totals[d0 + j] : 0;
+  // the words of smaller digits, and those of the digit before the tile, for digits
+  // that are consecutive over the threads
+  constexpr int kEach = kDigits / kBlock;
+  const int d0 = (int)threadIdx.x * kEach;
+  int total[kEach] = {}, before[kEach] = {}, own = 0;
+  if (p.tiles <= kFewTiles) {
+#pragma unroll 8
+    for (int t = 0; t < p.tiles; t++)
+#pragma unroll
+      for (int j = 0; j < kEach; j++) {
+        const int count = d0 + j < p.digits ? hist[(int64_t)t * p.digits + d0 + j] : 0;
+        total[j] += count;
+        before[j] += t < (int)blockIdx.x ? count : 0;
+      }
+  } else {
+#pragma unroll
+    for (int j = 0; j < kEach; j++)
+      if (d0 + j < p.digits) {
+        total[j] = totals[d0 + j];
+        before[j] = hist[(int64_t)blockIdx.x * p.digits + d0 + j];
+      }
+  }
+#pragma unroll
+  for (int j = 0; j < kEach; j++) own += total[j];
   const int upto = wave_prefix(own, lane);
   if (lane == kWave - 1) s_total[wave] = upto;
   __syncthreads();
   int base = upto - own;
   for (int w = 0; w < wave; w++) base += s_total[w];
-  for (int j = 0; j < each && d0 + j < p.digits; j++) {
+#pragma unroll
+  for (int j = 0; j < kEach; j++) {
     const int d = d0 + j;
-    int place = base + hist[(int64_t)d * p.tiles + blockIdx.x];
-    base += totals[d];
+    if (d >= p.digits) break;
+    int place = base + before[j];
+    base += total[j];
 #pragma unroll
     for (int w = 0; w < kTileWaves; w++) {
       const int count = s_next[w][d];
@@ -472,8 +519,7 @@ struct LaneColumns {
 };
 
 template <bool SHORT>
-__device__ __forceinline__ LaneColumns lane_columns(const Columns& c, int32_t D) {
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ LaneColumns lane_columns(const Columns& c, int32_t D, int lane) {
   const int pack = (int)blockIdx.y * c.lanes + lane;
   LaneColumns l;
   l.there = lane < c.lanes && pack * kE < D;
@@ -508,13 +554,13 @@ __device__ __forceinline__ void write_word(const EmbedBackwardArgs& a, uint32_t 
   }
 }
 
-// One wavefront a chunk of `chunk` (up to 64) sorted positions: the chunk's keys
-// are in its lanes, kAhead rows in flight. `head` and `tail`: partial sums of the
-// word that comes into the chunk from the one before, and of the one that goes
-// over its end and began within.
+// Rows of more than 256 elements: one wavefront a chunk of `chunk` (up to 64) sorted
+// positions, the chunk's keys in its lanes, kAhead rows in flight. `head` and `tail`:
+// partial sums of the word that comes into the chunk from the one before, and of the
+// one that goes over its end and began within.
 constexpr int kAhead = 8;
 
-template <typename TI, typename TG, bool SHORT>
+template <typename TI, typename TG>
 __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedBackwardArgs a, Columns cols,
                                                        const uint32_t* keys, const int32_t* at,
                                                        int chunk, float* head, float* tail) {
@@ -523,7 +569,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedBackwardArgs a, Colu
   const int64_t begin = k * chunk;
   if (begin >= a.n) return;
   const int size = (int)(a.n - begin < chunk ? a.n - begin : chunk);
-  const LaneColumns l = lane_columns<SHORT>(cols, a.D);
+  const LaneColumns l = lane_columns<false>(cols, a.D, (int)threadIdx.x & 63);
   const uint32_t V = (uint32_t)a.V;
   const uint32_t key = lane < size ? keys[begin + lane] : V;
   const int32_t row = lane < size ? at[begin + lane] : 0;
@@ -540,9 +586,9 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedBackwardArgs a, Colu
   const auto add = [&](const Pack<TI, kE>& in, uint32_t next) {
     if (next != word) {
       if (came) {
-        if (l.there) put<SHORT>(head + k * cols.ld + l.first, l.left, sum);
+        if (l.there) put<false>(head + k * cols.ld + l.first, l.left, sum);
       } else {
-        write_word<SHORT, TG>(a, word, l, sum);
+        write_word<false, TG>(a, word, l, sum);
       }
       word = next;
       came = false;
@@ -557,15 +603,74 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedBackwardArgs a, Colu
   for (; j0 + kAhead <= used; j0 += kAhead) {
     Pack<TI, kE> in[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; u++) in[u] = get_once<SHORT>(row_of(j0 + u), l.left);
+    for (int u = 0; u < kAhead; u++) in[u] = get_once<false>(row_of(j0 + u), l.left);
     // every load is under way before the first is waited for
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int u = 0; u < kAhead; u++) add(in[u], key_of(j0 + u));
   }
-  for (; j0 < used; j0++) add(get_once<SHORT>(row_of(j0), l.left), key_of(j0));
+  for (; j0 < used; j0++) add(get_once<false>(row_of(j0), l.left), key_of(j0));
   const bool goes = word == after;
   if (!came && !goes) {
+    write_word<false, TG>(a, word, l, sum);
+  } else if (l.there) {
+    put<false>((came ? head : tail) + k * cols.ld + l.first, l.left, sum);
+  }
+}
+
+// Shorter rows: TEAM lanes a chunk, as many as a row has packs, so that a wavefront
+// adds 2 to 8 rows at a time (10^6 rows of 64 bf16: 88 us with a wavefront a chunk).
+template <typename TI, typename TG, bool SHORT, int TEAM>
+__global__ __launch_bounds__(kBlock) void k_embed_team_sums(EmbedBackwardArgs a, Columns cols,
+                                                            const uint32_t* keys,
+                                                            const int32_t* at, int chunk,
+                                                            float* head, float* tail) {
+  const int64_t k = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / TEAM;
+  const bool any = k * chunk < a.n;
+  const int64_t begin = any ? k * chunk : 0;
+  const int size = !any ? 0 : (int)(a.n - begin < chunk ? a.n - begin : chunk);
+  const LaneColumns l = lane_columns<SHORT>(cols, a.D, (int)threadIdx.x & (TEAM - 1));
+  const uint32_t V = (uint32_t)a.V;
+  const uint32_t before = begin > 0 ? keys[begin - 1] : ~0u;
+  const uint32_t after = any && begin + size < a.n ? keys[begin + size] : ~0u;
+  const TI* dy = (const TI*)a.dy + l.first;
+  Pack<float, kE> sum{};
+  uint32_t word = any ? keys[begin] : V;
+  bool came = word == before;
+  // groups of kAhead lie within the arrays, which are of whole 256 bytes
+  Pack<uint32_t, kAhead> next_key = load_pack<uint32_t, kAhead>(keys + begin);
+  Pack<int32_t, kAhead> next_row = load_pack<int32_t, kAhead>(at + begin);
+  for (int j0 = 0; j0 < chunk; j0 += kAhead) {
+    const Pack<uint32_t, kAhead> key = next_key;
+    const Pack<int32_t, kAhead> row = next_row;
+    Pack<TI, kE> in[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; u++)
+      in[u] = get_once<SHORT>(dy + (j0 + u < size ? row.v[u] : 0) * a.lddy, l.left);
+    const int64_t from = j0 + kAhead < size ? begin + j0 + kAhead : begin;
+    next_key = load_pack<uint32_t, kAhead>(keys + from);
+    next_row = load_pack<int32_t, kAhead>(at + from);
+    // every load is under way before the first is waited for
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < kAhead; u++) {
+      if (j0 + u >= size || key.v[u] >= V) continue;  // absent words come last
+      if (key.v[u] != word) {
+        if (came) {
+          if (l.there) put<SHORT>(head + k * cols.ld + l.first, l.left, sum);
+        } else {
+          write_word<SHORT, TG>(a, word, l, sum);
+        }
+        word = key.v[u];
+        came = false;
+        sum = Pack<float, kE>{};
+      }
+#pragma unroll
+      for (int e = 0; e < kE; e++) sum.v[e] += to_f32(in[u].v[e]);
+    }
+  }
+  if (word >= V) return;
+  if (!came && word != after) {
     write_word<SHORT, TG>(a, word, l, sum);
   } else if (l.there) {
     put<SHORT>((came ? head : tail) + k * cols.ld + l.first, l.left, sum);
@@ -648,7 +753,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_spans(EmbedBackwardArgs a, Col
   if (first == 0 || last >= a.n) return;
   const uint32_t word = keys[first];
   if (word >= (uint32_t)a.V || keys[first - 1] != word || keys[last] != word) return;
-  const LaneColumns l = lane_columns<SHORT>(cols, a.D);
+  const LaneColumns l = lane_columns<SHORT>(cols, a.D, (int)threadIdx.x & 63);
   Pack<float, kE> sum{};
   add_rows<SHORT>(head + (int64_t)blockIdx.x * kSpan * cols.ld + l.first, cols.ld, kSpan,
                   threadIdx.x >> 6, kWaves, l.left, sum);
@@ -657,48 +762,59 @@ __global__ __launch_bounds__(kBlock) void k_embed_spans(EmbedBackwardArgs a, Col
 }
 
 // Joins the partial sums of the words that go over their chunk's end and began in
-// it: a wavefront a chunk, most of which have none, but all four of a block for
-// words over many chunks. In order: the word's own tail, the chunks up to a span,
-// the spans, the chunks behind.
+// it. A wavefront looks at `each` chunks at once (1 to 16) and joins what it finds one
+// after the other; words over many chunks are left to all four of a block. In order:
+// the word's own tail, the chunks up to a span, the spans, the chunks behind.
+constexpr int kMostEach = 16;
+
 template <typename TG, bool SHORT>
 __global__ __launch_bounds__(kBlock) void k_embed_join(EmbedBackwardArgs a, Columns cols,
                                                        const uint32_t* keys, int chunk,
-                                                       int64_t chunks, const float* head,
-                                                       const float* tail, const float* spans) {
+                                                       int64_t chunks, int each,
+                                                       const float* head, const float* tail,
+                                                       const float* spans) {
   constexpr int kAlone = 2 * kAhead;
   __shared__ float s_sum[kWaves][kWave][kE];
-  __shared__ int s_count[kWaves];  // chunks that the word of each wave's chunk goes on for
-  const int wave = threadIdx.x >> 6;
-  const LaneColumns l = lane_columns<SHORT>(cols, a.D);
-  for (int64_t k0 = (int64_t)blockIdx.x * kWaves; k0 + 1 < chunks; k0 += (int64_t)gridDim.x * kWaves) {
-    const int64_t k = k0 + wave, begin = k * chunk, end = begin + chunk;
-    uint32_t word = (uint32_t)a.V;
-    if (k + 1 < chunks) {
-      word = keys[end - 1];
-      const bool goes = word < (uint32_t)a.V && keys[end] == word;
-      const bool came = keys[begin] == word && begin > 0 && keys[begin - 1] == word;
-      if (!goes || came) word = (uint32_t)a.V;
-    }
-    int count = 0;
-    if (word < (uint32_t)a.V) count = (int)(last_chunk(keys, a.n, chunk, k, word) - k);
-    if (count > 0 && count <= kAlone) {
-      Pack<float, kE> sum = get<SHORT>(tail + k * cols.ld + l.first, l.left);
-      add_rows<SHORT>(head + (k + 1) * cols.ld + l.first, cols.ld, count, 0, 1, l.left, sum);
-      write_word<SHORT, TG>(a, word, l, sum);
+  __shared__ int s_long, s_chunk[kMostEach * kWaves], s_count[kMostEach * kWaves];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const LaneColumns l = lane_columns<SHORT>(cols, a.D, lane);
+  for (int64_t k0 = (int64_t)blockIdx.x * each * kWaves; k0 + 1 < chunks;
+       k0 += (int64_t)gridDim.x * each * kWaves) {
+    if (threadIdx.x == 0) s_long = 0;
+    __syncthreads();
+    const int64_t first = k0 + wave * each;
+    const bool looks = lane < each && first + lane + 1 < chunks;
+    const int64_t begin = looks ? (first + lane) * chunk : 0, end = looks ? begin + chunk : 1;
+    const uint32_t word = keys[end - 1], behind = keys[looks ? end : 0], own = keys[begin],
+                   before = keys[begin > 0 ? begin - 1 : 0];
+    const bool came = own == word && begin > 0 && before == word;
+    uint64_t found = __ballot(looks && word < (uint32_t)a.V && behind == word && !came);
+    for (; found != 0; found &= found - 1) {
+      const int at = __builtin_ctzll(found);
+      const uint32_t w = (uint32_t)__builtin_amdgcn_readlane((int)word, at);
+      const int64_t k = first + at;
+      const int count = (int)(last_chunk(keys, a.n, chunk, k, w) - k);
+      if (count <= kAlone) {
+        Pack<float, kE> sum = get<SHORT>(tail + k * cols.ld + l.first, l.left);
+        add_rows<SHORT>(head + (k + 1) * cols.ld + l.first, cols.ld, count, 0, 1, l.left, sum);
+        write_word<SHORT, TG>(a, w, l, sum);
+      } else if (lane == 0) {
+        const int to = atomicAdd(&s_long, 1);
+        s_chunk[to] = (int)(k - k0);
+        s_count[to] = count;
+      }
     }
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) s_count[wave] = count;
-    __syncthreads();
-    for (int w = 0; w < kWaves; w++) {
-      const int all = s_count[w];
-      if (all <= kAlone) continue;
-      const int64_t own = k0 + w, from = own + 1, to = from + all;
+    const int longs = s_long;
+    for (int i = 0; i < longs; i++) {
+      const int64_t own_chunk = k0 + s_chunk[i], from = own_chunk + 1, to = from + s_count[i];
       // a span with the word's last chunk, which it may not fill, has no sum
       int64_t g0 = (from + kSpan - 1) / kSpan, g1 = (to - 1) / kSpan;
       if (spans == nullptr || g1 <= g0) g0 = g1 = to / kSpan + 1;
       const int64_t stop = g0 * kSpan < to ? g0 * kSpan : to, on = g1 * kSpan < to ? g1 * kSpan : to;
       Pack<float, kE> sum{};
-      if (wave == 0) sum = get<SHORT>(tail + own * cols.ld + l.first, l.left);
+      if (wave == 0) sum = get<SHORT>(tail + own_chunk * cols.ld + l.first, l.left);
       add_rows<SHORT>(head + from * cols.ld + l.first, cols.ld, (int)(stop - from), wave, kWaves,
                       l.left, sum);
       if (g1 > g0)
@@ -707,9 +823,10 @@ __global__ __launch_bounds__(kBlock) void k_embed_join(EmbedBackwardArgs a, Colu
       add_rows<SHORT>(head + on * cols.ld + l.first, cols.ld, (int)(to - on), wave, kWaves, l.left,
                       sum);
       join_waves(s_sum, sum);
-      if (wave == 0) write_word<SHORT, TG>(a, keys[own * chunk + chunk - 1], l, sum);
+      if (wave == 0) write_word<SHORT, TG>(a, keys[own_chunk * chunk + chunk - 1], l, sum);
       __syncthreads();
     }
+    __syncthreads();
   }
 }
 
@@ -722,10 +839,13 @@ Columns columns_of(int32_t D) {
   return c;
 }
 
-// Long chunks leave few partial sums, short ones fill the card.
-int chunk_of(int32_t n) {
+// Lanes that add a chunk.
+int team_of(int32_t D) { return D <= 8 * kE ? 8 : D <= 16 * kE ? 16 : D <= 32 * kE ? 32 : kWave; }
+
+// Long chunks leave few partial sums, short ones fill the card with wavefronts.
+int chunk_of(int32_t n, int32_t D) {
   int chunk = kWave;
-  while (chunk > kAhead && (int64_t)n / chunk < 4096) chunk /= 2;
+  while (chunk > kAhead && (int64_t)n / chunk * team_of(D) / kWave < 4096) chunk /= 2;
   return chunk;
 }
 
@@ -755,7 +875,8 @@ Workspace lay_out(void* base, int32_t n, int32_t V, int32_t D) {
     used += aligned(bytes);
     return (void*)p;
   };
-  const int64_t chunks = ((int64_t)n + chunk_of(n) - 1) / chunk_of(n);
+  const int64_t chunks = ((int64_t)n + chunk_of(n, D) - 1) / chunk_of(n, D);
+  // of whole 256 bytes: read in groups of kAhead
   w.sorted = (uint32_t*)take(4 * (size_t)n);
   w.at = (int32_t*)take(4 * (size_t)n);
   const size_t row = 4 * (size_t)columns_of(D).ld;
@@ -800,22 +921,25 @@ void launch_order(const EmbedBackwardArgs& a, const Workspace& w, hipStream_t s)
   p.tiles = (int32_t)tiles_of(a.n);
   p.status = a.status;
   p.ids = a.ids;
-  const int launches = 3 * passes - 1;  // that clear: all behind the first
+  // that clear: all, or with marks all behind the first
+  const bool marks = !a.accumulate && a.n >= a.V / 8;
+  const int launches = (p.tiles > kFewTiles ? 3 : 2) * passes - (marks ? 1 : 0);
   int launch = 0;
-  const auto clear_next = [&]() {
+  const auto clear_next = [&](int threads = kBlock) {
     const int64_t first = (int64_t)a.V * launch / launches;
     launch++;
-    return clear_of(a, first, (int64_t)a.V * launch / launches, kBlock, w.taken);
+    return clear_of(a, first, (int64_t)a.V * launch / launches, threads,
+                    marks ? w.taken : nullptr);
   };
-  if (!a.accumulate) {
+  if (marks) {
     p.taken = w.taken;
-    // the marks, as a row of bytes of their own
-    EmbedBackwardArgs marks{};
-    marks.grad = w.taken;
-    marks.grad_dtype = W2V_DTYPE_BF16;
-    marks.V = (int32_t)(((int64_t)a.V + 511) / 512);
-    marks.D = marks.ldg = 256;
-    const Clear c = clear_of(marks, 0, marks.V);
+    // the marks' own zeros, as rows of 512 bytes
+    EmbedBackwardArgs none{};
+    none.grad = w.taken;
+    none.grad_dtype = W2V_DTYPE_BF16;
+    none.V = (int32_t)(((int64_t)a.V + 511) / 512);
+    none.D = none.ldg = 256;
+    const Clear c = clear_of(none, 0, none.V);
     hipLaunchKernelGGL(k_embed_clear, dim3(c.blocks), dim3(kBlock), 0, s, c);
   }
   for (int pass = 0; pass < passes; pass++) {
@@ -824,11 +948,13 @@ void launch_order(const EmbedBackwardArgs& a, const Workspace& w, hipStream_t s)
     const bool to_out = (passes - 1 - pass) % 2 == 0;
     uint32_t* keys = to_out ? w.sorted : w.keys;
     int32_t* at = to_out ? w.at : w.at_before;
-    Clear c = pass == 0 ? Clear{} : clear_next();
+    Clear c = marks && pass == 0 ? Clear{} : clear_next();
     hipLaunchKernelGGL(k_embed_count, dim3(p.tiles + c.blocks), dim3(kBlock), 0, s, p, w.hist, c);
-    c = clear_next();
-    hipLaunchKernelGGL(k_embed_scan, dim3(p.digits / kTileWaves + c.blocks), dim3(kBlock), 0, s,
-                       p, w.hist, w.totals, c);
+    if (p.tiles > kFewTiles) {
+      c = clear_next(kScanWaves * kWave);
+      hipLaunchKernelGGL(k_embed_scan, dim3((p.digits + kWave - 1) / kWave + c.blocks),
+                         dim3(kScanWaves * kWave), 0, s, p, w.hist, w.totals, c);
+    }
     c = clear_next();
     hipLaunchKernelGGL(k_embed_scatter, dim3(p.tiles + c.blocks), dim3(kBlock), 0, s, p, w.hist,
                        w.totals, keys, at, c);
@@ -842,21 +968,40 @@ void launch_order(const EmbedBackwardArgs& a, const Workspace& w, hipStream_t s)
 template <typename TI, typename TG, bool SHORT>
 hipError_t launch_sums(const EmbedBackwardArgs& a, const Workspace& w, hipStream_t s) {
   const Columns cols = columns_of(a.D);
-  const int chunk = chunk_of(a.n);
+  const int chunk = chunk_of(a.n, a.D);
   const int64_t chunks = ((int64_t)a.n + chunk - 1) / chunk;
   const unsigned tiles = (unsigned)cols.tiles;
-  hipLaunchKernelGGL((k_embed_sums<TI, TG, SHORT>), dim3((unsigned)((chunks + 3) / 4), tiles),
-                     dim3(kBlock), 0, s, a, cols, w.sorted, w.at, chunk, w.head, w.tail);
+  const int team = team_of(a.D), per_block = kBlock / team;
+  const dim3 grid((unsigned)((chunks + per_block - 1) / per_block), tiles);
+  const auto sums = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, s, a, cols, w.sorted, w.at, chunk, w.head,
+                       w.tail);
+  };
+  if constexpr (SHORT) {
+    sums(k_embed_team_sums<TI, TG, true, 8>);
+  } else if (team == 8) {
+    sums(k_embed_team_sums<TI, TG, false, 8>);
+  } else if (team == 16) {
+    sums(k_embed_team_sums<TI, TG, false, 16>);
+  } else if (team == 32) {
+    sums(k_embed_team_sums<TI, TG, false, 32>);
+  } else {
+    sums(k_embed_sums<TI, TG>);
+  }
   if (chunks == 1) return hipGetLastError();
   // spans shorten words over hundreds of chunks, for a launch
   const float* spans = chunks >= 64 * kSpan ? w.spans : nullptr;
   if (spans != nullptr)
     hipLaunchKernelGGL(k_embed_spans<SHORT>, dim3((unsigned)(chunks / kSpan), tiles), dim3(kBlock),
                        0, s, a, cols, w.sorted, chunk, w.head, w.spans);
-  const int64_t joins = (chunks - 1 + kWaves - 1) / kWaves;
+  // a wavefront a chunk while the card holds them (62,500 chunks, D 64: 41 us so, 30
+  // with 16 each; 3,125, D 300: 8 and 29)
+  int each = 1;
+  while (each < kMostEach && chunks / each > 16384) each *= 2;
+  const int64_t joins = (chunks - 1 + each * kWaves - 1) / (each * kWaves);
   hipLaunchKernelGGL((k_embed_join<TG, SHORT>),
                      dim3((unsigned)(joins < kMaxGrid ? joins : kMaxGrid), tiles), dim3(kBlock), 0,
-                     s, a, cols, w.sorted, chunk, chunks, w.head, w.tail, spans);
+                     s, a, cols, w.sorted, chunk, chunks, each, w.head, w.tail, spans);
   return hipGetLastError();
 }
 
