@@ -713,8 +713,8 @@ int w2v_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, v
  *   scales  bfloat16[ceil(N / 16)][G * 16]: of groups 4 i to 4 i + 3, [64 i + 4 r
  *           + j] is group 4 i + j's for row r, of the R others [64 (G / 4) + R r +
  *           j].
- * packed is 16-byte aligned and of w2v_q4_packed_bytes bytes, scales of
- * w2v_q4_scale_count elements (0 on invalid arguments). K <= 2^24.
+ * packed is of w2v_q4_packed_bytes bytes, scales of w2v_q4_scale_count elements
+ * (0 on invalid arguments), both 16-byte aligned. K <= 2^24.
  */
 size_t w2v_q4_packed_bytes(int32_t N, int32_t K, int32_t group);
 size_t w2v_q4_scale_count(int32_t N, int32_t K, int32_t group);
@@ -724,14 +724,15 @@ int w2v_quantize_q4(const void* w, int64_t ldw, int32_t N, int32_t K, int32_t dt
 /*
  * y = x W^T + bias for such a W, x M x K of `dtype` and y M x N of `out_dtype`
  * (dtype or W2V_DTYPE_F32); bias: device float[N] or NULL. Made for few rows:
- * the matrix is read once for every 64 of them (16-bit x) or 32 (fp32). Products
+ * the matrix is read once for every 64 of them (16-bit x) or 32 (fp32), for fewer
+ * where K is in the hundreds or more. Products
  * are exact and sums fp32: of a group, sum x (q + 16) - 24 sum x, so x whose
  * magnitudes add up to more than 2^122 in a group may overflow, and a row of x
  * with an infinity gives NaN. Each output is rounded once; the same call gives
  * the same bits. M = 0 is allowed and does nothing; M <= W2V_MAX_Q4_ROWS. y must
  * not overlap any other argument.
  */
-#define W2V_MAX_Q4_ROWS 1048576
+#define W2V_MAX_Q4_ROWS 524288
 
 int w2v_linear_q4(const void* x, int64_t ldx, const void* packed, const void* scales,
                   const float* bias, void* y, int64_t ldy, int32_t M, int32_t N, int32_t K,

@@ -42,9 +42,8 @@ int check_q4(int32_t N, int32_t K, int32_t group, int32_t dtype) {
 int check_packed(const void* packed, const void* scales) {
   if (packed == nullptr) return fail(W2V_EINVAL, "packed is NULL");
   if (scales == nullptr) return fail(W2V_EINVAL, "scales is NULL");
-  if ((uintptr_t)packed % 16 != 0) return fail(W2V_EINVAL, "packed must be 16-byte aligned");
-  if ((uintptr_t)scales % 2 != 0)
-    return fail(W2V_EINVAL, "scales must be aligned to its elements");
+  if (((uintptr_t)packed | (uintptr_t)scales) % 16 != 0)
+    return fail(W2V_EINVAL, "packed and scales must be 16-byte aligned");
   return W2V_OK;
 }
 

@@ -985,7 +985,7 @@ def quantize_q4(weight, *, group: int = 32, stream=None):
 
 def linear_q4(x, weight, bias=None, *, out_dtype=None, out=None, stream=None):
     """x W^T + bias for a W of quantize_q4() (w2v_linear_q4), which is read once
-    for every 64 rows of x (32 of float32).
+    for every 64 rows of x or fewer.
 
     x (M, K) float32, bfloat16 or float16, rows may be padded; bias float32
     (N,). out_dtype: x's type (the default) or float32. out: receives the

@@ -75,7 +75,7 @@ def test_dropout_rejects(over, needle, code):
     (dict(N=0), "N"), (dict(K=0), "K"), (dict(group=16), "group"), (dict(group=0), "group"),
     (dict(dtype=3), "dtype"), (dict(w=None), "w is NULL"), (dict(ldw=7), "w: the row"),
     (dict(packed=None), "packed"), (dict(packed=FAKE + 8), "packed"), (dict(scales=None), "scales"),
-    (dict(scales=FAKE + 1), "scales"),
+    (dict(scales=FAKE + 1), "scales"), (dict(scales=FAKE + 2), "16-byte"),
 ])
 def test_quantize_rejects(over, needle):
     args = dict(w=FAKE, ldw=8, N=4, K=8, dtype=0, group=32, packed=FAKE, scales=FAKE, stream=None)
@@ -88,7 +88,7 @@ def test_quantize_rejects(over, needle):
     (dict(K=0), "K", -1), (dict(group=96), "group", -1), (dict(dtype=3), "dtype", -1),
     (dict(out=1), "out_dtype", -1), (dict(dtype=1, out=2), "out_dtype", -1),
     (dict(x=None), "x", -1), (dict(ldx=7), "x: the row", -1), (dict(packed=None), "packed", -1),
-    (dict(scales=FAKE + 1), "scales", -1), (dict(y=None), "y", -1), (dict(ldy=4), "y: the row", -1),
+    (dict(scales=FAKE + 2), "scales", -1), (dict(y=None), "y", -1), (dict(ldy=4), "y: the row", -1),
     (dict(bias=FAKE + 2), "bias", -1), (dict(K=(1 << 24) + 1, ldx=1 << 25), "K must", -4),
 ])
 def test_linear_q4_rejects(over, needle, code):

@@ -249,6 +249,36 @@ def test_numbers_that_are_not_finite():
         assert torch.isnan(w2v.beam_step(z, scores)["scores"][4]).all()
 
 
+def test_masks_of_the_lowest_number():
+    """Words at the type's lowest number are words still, behind all others."""
+    import torch
+    g = generator(13)
+    for name in NAMES:
+        z, scores = inputs(g, 2, 3, 4000, name)
+        low = torch.finfo(z.dtype).min
+        z[:, 5:] = low
+        out = w2v.beam_step(z, scores, width=20)
+        check(z, scores, out, 20)
+        assert (out["words"][:, :15] < 5).all()
+        z[:] = low
+        out = w2v.beam_step(z, scores, width=2)
+        assert (out["words"] == torch.arange(2, device="cuda")).all()
+
+
+def test_rows_beyond_32_bit_offsets():
+    """Scores past 2^32 elements."""
+    import torch
+    V = 1_049_000
+    z = torch.zeros((4096, V), dtype=torch.bfloat16, device="cuda")
+    scores = torch.full((64, 64), -50.0, device="cuda")
+    scores[:, 63] = 0.0
+    z[63::64, V - 1] = 9.0
+    z[63::64, 77] = 8.0
+    out = w2v.beam_step(z, scores, width=3)
+    assert out["words"].tolist() == [[V - 1, 77, 0]] * 64
+    assert (out["parents"] == 63).all()
+
+
 def test_probabilities_add_up():
     """One beam, as wide as the vocabulary: the scores are its log-probabilities."""
     import torch

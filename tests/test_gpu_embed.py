@@ -137,7 +137,8 @@ def check_back(dy, ids, out, V, scale, old=None):
 @pytest.mark.parametrize("n,V,D,pad", [
     (1, 1, 1, 0), (1, 1000, 300, 0), (9, 4, 7, 3), (70, 1, 64, 0), (500, 30, 9, 1),
     (3000, 700, 300, 20), (8192, 5, 16, 0), (8193, 5, 16, 0), (20_000, 3000, 33, 0),
-    (600, 40, 513, 0), (300, 70, 1100, 7)])
+    (600, 40, 513, 0), (300, 70, 1100, 7), (3000, 50, 100, 0), (2500, 700, 128, 1),
+    (9001, 90, 200, 0), (2500, 9, 256, 0), (2500, 9, 257, 3), (70_001, 60_000, 72, 0)])
 def test_gradient(name, grad, n, V, D, pad):
     g = generator(3 * n + D)
     ids, dy = words(g, n, V).cuda(), matrix(g, n, D, name, pad=pad)
@@ -157,7 +158,8 @@ def test_gradient(name, grad, n, V, D, pad):
 
 
 @pytest.mark.parametrize("n,V", [(40_000, 1), (300_000, 2), (300_000, 1_000_000),
-                                 (100_003, 65_536), (66_000, 63)])
+                                 (100_003, 65_536), (66_000, 63), (65_536, 1_500_000),
+                                 (65_537, 3), (9_000, 1_048_576), (1_200_000, 70_000)])
 def test_long_runs_of_one_word(n, V):
     """A word over many chunks, words whose runs end at a chunk's end, and a
     vocabulary of several digits."""

@@ -140,12 +140,15 @@ def test_products(name, group, M, N, K):
     assert untouched()
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("name,M,K", [("float32", 5, 9001), ("bfloat16", 40, 9001),
-                                      ("float16", 64, 4500), ("float32", 20, 4500)])
-def test_long_sums(name, M, K):
-    """More columns than LDS holds of x at once."""
+                                      ("float16", 64, 4500), ("float32", 20, 4500),
+                                      ("float32", 40, 700), ("bfloat16", 64, 1100),
+                                      ("float16", 20, 2100), ("float32", 3, 1000)])
+def test_long_sums(name, M, K, group):
+    """More columns than LDS holds of x at once, or of all of its rows."""
     g = generator(K)
-    q = random_q4(g, 70, K, 32)
+    q = random_q4(g, 70, K, group)
     x = matrix(g, M, K, name)
     check(x, q, w2v.linear_q4(x, q))
 
