@@ -1,5 +1,8 @@
 """A word model's ends together with the vocabulary head: a training step from
 words to gradients, and a search over scores from 4-bit weights."""
+import importlib.util
+import os
+
 import pytest
 
 from ends_util import captured, generator, matrix
@@ -7,6 +10,7 @@ from paper_1611_06172_amd import w2v
 
 pytestmark = pytest.mark.gpu
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 V, D, N, K = 3001, 40, 150, 12
 
 
@@ -154,3 +158,42 @@ def test_search_replayed_from_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held, eager))
+
+
+def example():
+    spec = importlib.util.spec_from_file_location(
+        "next_words", os.path.join(ROOT, "examples", "next_words.py"))
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+def test_example_runs():
+    import torch
+    losses, words, scores = example().main(V=500, topics=10, T=20_000, D=48, steps=12, batch=256,
+                                           verbose=False)
+    assert torch.isfinite(losses).all() and torch.isfinite(scores).all()
+    assert words.shape == (4, 4, 6) and (words >= 0).all() and (words < 500).all()
+    assert (scores <= 0).all() and (scores[:, 1:] <= scores[:, :-1]).all()
+
+
+def test_example_gradients():
+    """Against autograd in 64 bits, with the mask that the step draws; the bound as
+    in test_gradients_of_a_step."""
+    import torch
+    model = example().Model(400, 40, p=0.3)
+    g = generator(8)
+    words = torch.randint(-1, 400, (90,), generator=g, dtype=torch.int32)
+    labels = torch.randint(-1, 400, (90,), generator=g, dtype=torch.int32)
+    model.b.copy_(torch.randn(40, generator=g))
+    model.c.copy_(torch.randn(400, generator=g))
+    loss, grads = model.gradients(words.cuda(), labels.cuda(), 17)
+    keep = (w2v.dropout(torch.ones((90, 40), device="cuda"), 0.3, seed=3, offset=17) > 0).cpu()
+    E, W, b, c = (t.cpu().double().requires_grad_() for t in (model.E, model.W, model.b, model.c))
+    x = E[words.long().clamp(min=0)] * 40 ** 0.5 * (words >= 0)[:, None] * keep / 0.7
+    lp = torch.log_softmax((x + torch.nn.functional.gelu(x @ W.t() + b)) @ E.t() + c, 1)
+    want = -lp[torch.arange(90), labels.long().clamp(min=0)] * (labels >= 0)
+    want.mean().backward()
+    assert (loss.cpu().double() - want.detach()).abs().max() <= 1e-4 * want.max()
+    for name, t in (("E", E), ("W", W), ("b", b), ("c", c)):
+        assert (grads[name].cpu().double() - t.grad).abs().max() <= 1e-4 * t.grad.abs().max()
