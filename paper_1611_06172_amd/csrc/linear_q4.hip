@@ -360,15 +360,19 @@ struct Tiles {
   }
 };
 
-// Wavefronts of a SIMD that the registers are to allow.
-constexpr int resident_waves(int mt) { return mt == 1 ? 4 : mt == 2 ? 3 : 2; }
+// Wavefronts of a SIMD that the registers are to allow, 128 each. That takes one tile
+// of W at a time with several of x (61 x 100,000 x 600 fp16 in groups of 64: 23 us,
+// with two at 2 wavefronts 26); with one of x, two share its readings from LDS (16 x
+// 10^6 x 300 fp32: 61, with one 65).
+constexpr int kResident = 4;
+constexpr int tiles_at_once(int mt) { return mt == 1 ? 2 : 1; }
 
 // One block: sets of WAVES x NT tiles of W, against MT tiles of x (blockIdx.y).
 // `span` blocks of columns of x are in LDS at once; where that is all of them (ONCE)
 // they are put there once. A wavefront goes through its steps of all sets with the next
 // one's loads on their way.
 template <typename T, int MT, int NT, int GB, int WAVES, bool ONCE>
-__global__ __launch_bounds__(WAVES* kWave, resident_waves(MT)) void k_linear_q4(LinearQ4Args a, Q4Shape q, int span) {
+__global__ __launch_bounds__(WAVES* kWave, kResident) void k_linear_q4(LinearQ4Args a, Q4Shape q, int span) {
   extern __shared__ uint4 frags[];
   float* sums = (float*)(frags + (int64_t)span * MT * Operand<T>::kPieces * kWave);
   const int lane = threadIdx.x & 63, r = lane & 15;
@@ -470,12 +474,12 @@ int most_blocks(int mt, int group) {
 
 template <typename T, int MT, int GB, int WAVES, bool ONCE>
 hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, int span, hipStream_t s) {
-  constexpr int NT = 2;
+  constexpr int NT = tiles_at_once(MT);
   const int bytes = span * block_bytes<T>(MT, GB);
   const int64_t sets = (q.tiles + WAVES * NT - 1) / (WAVES * NT);
   // as many blocks as the card holds at once, so that all end at the same time:
   // each puts x into LDS for itself
-  const int64_t by_lds = kLds / bytes, by_registers = resident_waves(MT) * 4 / WAVES;
+  const int64_t by_lds = kLds / bytes, by_registers = kResident * 4 / WAVES;
   const int64_t fit = 256 * (by_lds < by_registers ? by_lds : by_registers);
   const dim3 grid((unsigned)(sets < fit ? sets : fit), (unsigned)((a.M + MT * 16 - 1) / (MT * 16)));
   if (bytes > (64 << 10)) {
@@ -493,11 +497,11 @@ hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, int span, hipStream_t
 // 37 us with four of 16.
 template <typename T, int MT, int GB>
 hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
-  constexpr int kAll = resident_waves(MT) * 4;
+  constexpr int kAll = kResident * 4;
   const int most = most_blocks<T>(MT, GB * 32);
   if (q.blocks > most) return launch<T, MT, GB, kAll, false>(a, q, most, s);
-  if (MT < 4 && q.blocks * block_bytes<T>(MT, GB) <= kLds / resident_waves(MT))
-    return launch<T, MT, GB, MT < 4 ? 4 : kAll, true>(a, q, q.blocks, s);
+  if (q.blocks * block_bytes<T>(MT, GB) <= kLds / kResident)
+    return launch<T, MT, GB, 4, true>(a, q, q.blocks, s);
   return launch<T, MT, GB, kAll, true>(a, q, q.blocks, s);
 }
 
