@@ -27,6 +27,7 @@ constexpr int kBlock = 256;
 constexpr int kWaves = kBlock / kWave;
 constexpr int kMaxGrid = 1 << 22;
 constexpr int kList = 1024;
+constexpr int kPackList = 512;
 constexpr float kInf = __builtin_inff();
 
 __device__ __forceinline__ bool live_score(float c) { return c > -kInf; }  // not NaN
@@ -75,7 +76,7 @@ struct Bound {
     if ((int)threadIdx.x >= count) return;
     const float mine = groups[threadIdx.x];
     int above = 0;
-#pragma unroll 8
+#pragma unroll 2
     for (int i = 0; i < count; i += 4) {
       const f32x4 o = *(const f32x4*)(groups + i);
       above += (o[0] > mine) + (o[1] > mine) + (o[2] > mine) + (o[3] > mine);
@@ -95,43 +96,88 @@ template <typename T, int PACKS>
 struct Row {
   static constexpr int kE = 16 / (int)sizeof(T);
   static constexpr int kShare = kBlock * PACKS * kE;
-  uint4 w[PACKS];
+  word4 w[PACKS];
 
+  __device__ __forceinline__ static word4 load(const T* p) {
+    return __builtin_bit_cast(word4, load_16(p));
+  }
   // Elements [first, first + kShare) of the n of a row; -inf past its end.
   __device__ __forceinline__ void load(const T* row, int64_t first, int64_t n) {
     const int64_t mine = first + threadIdx.x * kE;
     if (first + kShare <= n) {
 #pragma unroll
-      for (int p = 0; p < PACKS; p++) w[p] = load_16(row + mine + p * kBlock * kE);
+      for (int p = 0; p < PACKS; p++) w[p] = load(row + mine + p * kBlock * kE);
       return;
+    }
+    // the row's last pack, where it is not whole
+    const int64_t whole = n - n % kE;
+    Pack<T, kE> tail, gone;
+#pragma unroll
+    for (int e = 0; e < kE; e++) {
+      gone.v[e] = from_f32<T>(-kInf);
+      tail.v[e] = whole + e < n ? row[whole + e] : gone.v[e];
     }
 #pragma unroll
     for (int p = 0; p < PACKS; p++) {
       const int64_t i = mine + p * kBlock * kE;
-      if (i + kE <= n) {
-        w[p] = load_16(row + i);
-      } else {
-        Pack<T, kE> some;
-#pragma unroll
-        for (int e = 0; e < kE; e++) some.v[e] = i + e < n ? row[i + e] : from_f32<T>(-kInf);
-        w[p] = __builtin_bit_cast(uint4, some);
-      }
+      if (i < whole)
+        w[p] = load(row + i);
+      else
+        w[p] = __builtin_bit_cast(word4, i < n ? tail : gone);
     }
   }
   // Keeps the compiler from holding what one reading unpacked for the next: 8
   // registers a pack instead of 4, and two wavefronts a SIMD instead of five.
-  __device__ __forceinline__ void repack() {
-#pragma unroll
-    for (int p = 0; p < PACKS; p++)
-      asm volatile("" : "+v"(w[p].x), "+v"(w[p].y), "+v"(w[p].z), "+v"(w[p].w));
+  __device__ __forceinline__ void repack(int p) {
+    asm volatile("" : "+v"(w[p]));
   }
-  // f(score, index in the share), in order of the index
+  // The largest score of pack p, of NaN's others.
+  __device__ __forceinline__ float most(int p) {
+    float z[kE];
+    repack(p);
+    unpack_words<T>(__builtin_bit_cast(uint4, w[p]), z);
+    float m = fmaxf(z[0], z[1]);
+#pragma unroll
+    for (int e = 2; e < kE; e += 2) m = fmaxf(m, fmaxf(z[e], z[e + 1]));
+    asm volatile("" : "+v"(m));
+    return m;
+  }
+  // Sum of exp(z - top). Of fp16 exp2(z k - t), t the rounded top k, is one
+  // instruction before the exponential, with the conversion, where exp2((z - top) k)
+  // takes three; that sum is 2^(top k - t) times too large or small, at most
+  // 1 +- 0.006 as no fp16 is over 2^16, and the series of that factor is off by 4e-11.
+  __device__ __forceinline__ float sum_exp(float top) {
+    float sum = 0.0f;
+    if constexpr (__is_same(T, f16_t)) {
+      const float t = top * kLog2e;
+      add(sum, [&](float v) { return fmaf(v, kLog2e, -t); });
+      const float x = fmaf(-kLog2e, top, t) * 0.6931471805599453f;
+      return fmaf(sum, fmaf(x * x, fmaf(x, 1.0f / 6, 0.5f), x), sum);
+    } else {
+      add(sum, [&](float v) { return (v - top) * kLog2e; });
+      return sum;
+    }
+  }
   template <typename F>
-  __device__ __forceinline__ void each(F&& f) const {
+  __device__ __forceinline__ void add(float& sum, F&& power) {
 #pragma unroll
     for (int p = 0; p < PACKS; p++) {
       float z[kE];
-      unpack_words<T>(w[p], z);
+      repack(p);
+      unpack_words<T>(__builtin_bit_cast(uint4, w[p]), z);
+#pragma unroll
+      for (int e = 0; e < kE; e++) sum += exp2_fast(power(z[e]));
+      asm volatile("" : "+v"(sum));
+    }
+  }
+  // f(score, index in the share), in order of the index
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) {
+#pragma unroll
+    for (int p = 0; p < PACKS; p++) {
+      float z[kE];
+      repack(p);
+      unpack_words<T>(__builtin_bit_cast(uint4, w[p]), z);
       int first = (int)threadIdx.x * kE;
       asm volatile("" : "+v"(first));  // not an index for each element at once
 #pragma unroll
@@ -141,13 +187,16 @@ struct Row {
 };
 
 template <typename T, int PACKS>
-__global__ __launch_bounds__(kBlock) void k_beam_shares(BeamArgs a, int shares, Share* out,
+__global__ __launch_bounds__(kBlock, 4) void k_beam_shares(BeamArgs a, int shares, Share* out,
                                                         Word* best) {
   __shared__ __attribute__((aligned(16))) Bound s_bound;
   __shared__ float s_wave[2 * kWaves];
-  __shared__ int s_count;
+  __shared__ int s_packs, s_count;
+  __shared__ word4 s_pack[kPackList];
+  __shared__ int s_first[kPackList];
   __shared__ Word s_list[kList];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int kE = Row<T, PACKS>::kE;
   const int64_t units = (int64_t)a.batch * a.beams * shares;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const int64_t row = unit / shares;
@@ -157,35 +206,54 @@ __global__ __launch_bounds__(kBlock) void k_beam_shares(BeamArgs a, int shares, 
     const int64_t first = (unit - row * shares) * Row<T, PACKS>::kShare;
     Row<T, PACKS> z;
     z.load((const T*)a.logits + row * a.ld, first, a.V);
-    float most = -kInf;
-    z.each([&](float v, int) { most = fmaxf(most, v); });
+    // the largest of every kPer packs, so that the others are not read for words
+    constexpr int kPer = PACKS > 1 ? 2 : 1;
+    float most = -kInf, of_packs[PACKS / kPer];
+#pragma unroll
+    for (int p = 0; p < PACKS; p += kPer) {
+      float m = z.most(p);
+      if constexpr (kPer > 1) m = fmaxf(m, z.most(p + 1));
+      most = fmaxf(most, of_packs[p / kPer] = m);
+    }
     s_bound.begin(most, a.width);
     const float of_wave = wave_max(most);
     if (lane == 0) s_wave[wave] = of_wave;
-    if (threadIdx.x == 0) s_count = 0;
+    if (threadIdx.x == 0) s_packs = s_count = 0;
     __syncthreads();
     most = s_wave[0];
 #pragma unroll
     for (int w = 1; w < kWaves; w++) most = fmaxf(most, s_wave[w]);
     s_bound.end(a.width);
     // a share of -inf alone has sum 0; NaN and +inf make it NaN
-    z.repack();
-    float sum = 0.0f;
-    const float top = most > -kInf ? most : 0.0f;
-    z.each([&](float v, int) { sum += exp2_fast((v - top) * kLog2e); });
-    sum = wave_sum(sum);
+    float sum = wave_sum(z.sum_exp(most > -kInf ? most : 0.0f));
     if (lane == 0) s_wave[kWaves + wave] = sum;
     __syncthreads();
-    const float bound = s_bound.get(a.width);
-    z.repack();
-    z.each([&](float v, int i) {
-      if (v >= bound && v > -kInf) {
-        const int at = atomicAdd(&s_count, 1);
-        if (at < kList) s_list[at] = {v, i};
+    // the packs that hold words to take, then those words; of a NaN neither
+    const float bound = fmaxf(s_bound.get(a.width), -__FLT_MAX__);
+#pragma unroll
+    for (int p = 0; p < PACKS; p += kPer)
+      if (of_packs[p / kPer] >= bound) {
+        const int at = atomicAdd(&s_packs, kPer);
+        if (at <= kPackList - kPer) {
+#pragma unroll
+          for (int u = 0; u < kPer; u++) {
+            s_pack[at + u] = z.w[p + u];
+            s_first[at + u] = ((p + u) * kBlock + (int)threadIdx.x) * kE;
+          }
+        }
       }
-    });
     __syncthreads();
-    const int count = s_count;
+    const int packs = s_packs;
+    if (packs <= kPackList)
+      for (int i = threadIdx.x; i < packs * kE; i += kBlock) {
+        const float v = to_f32(((const T*)s_pack)[i]);
+        if (v >= bound) {
+          const int at = atomicAdd(&s_count, 1);
+          if (at < kList) s_list[at] = {v, s_first[i / kE] + i % kE};
+        }
+      }
+    __syncthreads();
+    const int count = packs <= kPackList ? s_count : kList + 1;
     Word* to = best + unit * a.width;
     if (count <= kList) {
       for (int i = threadIdx.x; i < count; i += kBlock) {
@@ -199,7 +267,6 @@ __global__ __launch_bounds__(kBlock) void k_beam_shares(BeamArgs a, int shares, 
     } else {
       Word last = {kInf, -1};
       for (int i = 0; i < a.width; i++) {
-        z.repack();
         Word mine = {-kInf, 0x7fffffff};
         z.each([&](float v, int id) {
           if (v > mine.z && better(last, {v, id})) mine = {v, id};
