@@ -54,16 +54,20 @@ __device__ __forceinline__ Word best_of_wave(Word w) {
 }
 
 // The n-th largest of the maxima of 64 groups of four threads, or of all threads'
-// values for n > 16, by counting the larger ones: what at least n values of the
-// block's threads reach. begin() and, behind a barrier, end() of all threads; the
+// values for n > 16 or ALL, by counting the larger ones: what at least n values of
+// the block's threads reach. begin() and, behind a barrier, end() of all threads; the
 // result is there behind another one.
 struct Bound {
   float groups[kBlock];
   float waves[kWaves];
 
-  __device__ __forceinline__ static bool few(int n) { return n <= 16; }
+  template <bool ALL>
+  __device__ __forceinline__ static bool few(int n) {
+    return !ALL && n <= 16;
+  }
+  template <bool ALL = false>
   __device__ __forceinline__ void begin(float v, int n) {
-    if (few(n)) {
+    if (few<ALL>(n)) {
       v = fmaxf(v, __shfl_xor(v, 1));
       v = fmaxf(v, __shfl_xor(v, 2));
       if ((threadIdx.x & 3) == 0) groups[threadIdx.x >> 2] = v;
@@ -71,8 +75,9 @@ struct Bound {
       groups[threadIdx.x] = v;
     }
   }
+  template <bool ALL = false>
   __device__ __forceinline__ void end(int n) {
-    const int count = few(n) ? kBlock / 4 : kBlock;
+    const int count = few<ALL>(n) ? kBlock / 4 : kBlock;
     if ((int)threadIdx.x >= count) return;
     const float mine = groups[threadIdx.x];
     int above = 0;
@@ -84,9 +89,10 @@ struct Bound {
     const float least = -wave_max(above < n ? -mine : -kInf);
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = least;
   }
+  template <bool ALL = false>
   __device__ __forceinline__ float get(int n) const {
     float least = waves[0];
-    if (!few(n))
+    if (!few<ALL>(n))
       for (int w = 1; w < kWaves; w++) least = fminf(least, waves[w]);
     return least;
   }
@@ -410,22 +416,56 @@ __global__ __launch_bounds__(kBlock) void k_beam_merge(BeamArgs a, int shares, c
         }
       }
     __syncthreads();
-    const int hot = s_hot;
-    for (int i = threadIdx.x; i < hot * a.width && hot <= kList; i += kBlock) {
-      const int at = i / a.width;
-      const Pair p = pair_of(s_lists[at], i - at * a.width);
-      if ((float)p.key >= bound && p.key > -(double)kInf) {
-        const int to = atomicAdd(&s_count, 1);
-        if (to < kList) {
-          s_list[to] = p;
-          s_key[to] = p.key;
-          s_tie[to] = (uint64_t)p.beam << 32 | (uint32_t)p.id;
-          s_z[to] = p.z;
-        }
+    const auto put = [&](const Pair& p) {
+      const int to = atomicAdd(&s_count, 1);
+      s_list[to] = p;
+      s_key[to] = p.key;
+      s_tie[to] = (uint64_t)p.beam << 32 | (uint32_t)p.id;
+      s_z[to] = p.z;
+    };
+    // They are taken into a list of kList, as many at a time as it has room for. Many
+    // of them give a closer bound, the width-th largest of what the threads hold, and
+    // those below it leave the list: 16 of 174 are ranked in 3 us, with the bound, 174
+    // in 9. Equal scores can fill the list.
+    const int hot = s_hot, words = hot <= kList ? hot * a.width : 0;
+    int count = 0;
+    float least = bound;
+    for (int from = 0; from < words && count <= kList / 2;) {
+      const int stop = words - from < kList - count ? words : from + kList - count;
+      for (int i = from + (int)threadIdx.x; i < stop; i += kBlock) {
+        const int at = i / a.width;
+        const Pair p = pair_of(s_lists[at], i - at * a.width);
+        if ((float)p.key >= least && p.key > -(double)kInf) put(p);
       }
+      from = stop;
+      __syncthreads();
+      count = s_count;
+      if (count > 4 * a.width) {
+        Pair p[kList / kBlock];
+        float most = -kInf;
+#pragma unroll
+        for (int u = 0; u < kList / kBlock; u++) {
+          const int i = u * kBlock + (int)threadIdx.x;
+          p[u] = none;
+          if (i < count) p[u] = s_list[i];
+          most = fmaxf(most, (float)p[u].key);
+        }
+        s_bound.begin<true>(most, a.width);
+        __syncthreads();
+        if (threadIdx.x == 0) s_count = 0;
+        s_bound.end<true>(a.width);
+        __syncthreads();
+        least = s_bound.get<true>(a.width);
+#pragma unroll
+        for (int u = 0; u < kList / kBlock; u++)
+          if ((float)p[u].key >= least && p[u].key > -(double)kInf) put(p[u]);
+        __syncthreads();
+        count = s_count;
+      }
+      __syncthreads();
+      if (from < words && count > kList / 2) count = kList + 1;
     }
-    __syncthreads();
-    const int count = hot <= kList ? s_count : kList + 1;
+    if (hot > kList) count = kList + 1;
     // pairs are compared in fours
     if (count <= kList && threadIdx.x < 4) s_key[count + threadIdx.x] = none.key;
     __syncthreads();

@@ -219,6 +219,22 @@ def test_best_words_in_few_threads(name, width):
         check(z, scores, w2v.beam_step(z, scores, width=width), width)
 
 
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("apart", [0.0, 0.02, 3.0])
+def test_many_wide_beams(name, apart):
+    """Beams alike and beams of which one has nearly all continuations: more words
+    above the first bound than the merge's list holds at once."""
+    import torch
+    g = generator(31)
+    for V in (9_000, 70_000):
+        z = matrix(g, 128, V, name, scale=1.0)
+        scores = (-apart * torch.arange(64.0)).expand(2, 64).contiguous().cuda()
+        out = w2v.beam_step(z, scores, width=64)
+        check(z, scores, out, 64)
+        again = w2v.beam_step(z, scores, width=64)
+        assert all((again[k] == out[k]).all() for k in ("words", "parents", "scores"))
+
+
 def test_lists_that_hold_nothing():
     """Words in one share alone: most of the lists are empty."""
     import torch
