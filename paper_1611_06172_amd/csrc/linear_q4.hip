@@ -314,8 +314,9 @@ template <int NT, int GB>
 struct Tiles {
   __amdgpu_buffer_rsrc_t words, scales, bias;
 
-  __device__ __forceinline__ void begin(const LinearQ4Args& a, const Q4Shape& q, int64_t tile) {
-    const int64_t left = q.tiles - tile;
+  __device__ __forceinline__ void begin(const LinearQ4Args& a, const Q4Shape& q, int64_t tile,
+                                        int64_t end) {
+    const int64_t left = end - tile;
     const int count = left >= NT ? NT : left > 0 ? (int)left : 0;
     const int64_t rows = q.N - tile * 16;
     words = checked(a.packed + tile * q.blocks * 64, count * q.blocks * 256);
@@ -365,12 +366,18 @@ struct Tiles {
 // with two at 2 wavefronts 26); with one of x, two share its readings from LDS (16 x
 // 10^6 x 300 fp32: 61, with one 65).
 constexpr int kResident = 4;
+constexpr int kAll = 4 * kResident;
 constexpr int tiles_at_once(int mt) { return mt == 1 ? 2 : 1; }
 
-// One block: sets of WAVES x NT tiles of W, against MT tiles of x (blockIdx.y).
-// `span` blocks of columns of x are in LDS at once; where that is all of them (ONCE)
-// they are put there once. A wavefront goes through its steps of all sets with the next
-// one's loads on their way.
+// One block: NT tiles of W at a time and wavefront, against MT tiles of x
+// (blockIdx.y). `span` blocks of columns of x are in LDS at once; where that is all of
+// them (ONCE) they are put there once, and the wavefronts do not wait for each other.
+// A wavefront goes through the steps of all its tiles with the next one's loads on
+// their way.
+// Small blocks take sets of neighbouring tiles in turn: W is read in its order (16 x
+// 10^6 x 300 fp32 61 us, each block with a stretch of its own 64). Large ones, one a
+// CU, take a stretch each, all of one length: 391 sets for 256 blocks would be two
+// rounds (61 x 100,000 x 600 fp16 in groups of 64: 23.0 to 21.7 us).
 template <typename T, int MT, int NT, int GB, int WAVES, bool ONCE>
 __global__ __launch_bounds__(WAVES* kWave, kResident) void k_linear_q4(LinearQ4Args a, Q4Shape q, int span) {
   extern __shared__ uint4 frags[];
@@ -378,23 +385,35 @@ __global__ __launch_bounds__(WAVES* kWave, kResident) void k_linear_q4(LinearQ4A
   const int lane = threadIdx.x & 63, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m0 = blockIdx.y * MT * 16;
-  const int64_t sets = (q.tiles + WAVES * NT - 1) / (WAVES * NT);
+  const int64_t b = blockIdx.x;
+  int64_t first = b * WAVES * NT, end = q.tiles, step = (int64_t)gridDim.x * WAVES * NT;
+  if (WAVES == kAll) {
+    const int64_t units = (q.tiles + NT - 1) / NT, each = units / gridDim.x;
+    const int64_t more = units - each * gridDim.x;
+    first = (b * each + (b < more ? b : more)) * NT;
+    end = first + (each + (b < more)) * NT;
+    if (end > q.tiles) end = q.tiles;
+    step = WAVES * NT;
+  }
   f32x4 acc[NT][MT] = {};
-  // where the loads and the products are
-  int64_t load_set = blockIdx.x, set = blockIdx.x;
+  // where the loads and the products are, of the wavefront itself or of the block's
+  // first one
+  const int64_t start = ONCE ? first + wave * NT : first;
+  const int own = ONCE ? 0 : wave * NT;
+  int64_t load_tile = start, tile0 = start;
   int load_block = 0, block = 0;
   Tiles<NT, GB> tiles;
-  tiles.begin(a, q, (load_set * WAVES + wave) * NT);
-  const auto load = [&](Step<NT, GB>& step) {
-    tiles.load(q, load_block, step);
+  tiles.begin(a, q, load_tile + own, end);
+  const auto load = [&](Step<NT, GB>& to) {
+    tiles.load(q, load_block, to);
     load_block += 4;
     if (load_block >= q.blocks) {
       load_block = 0;
-      load_set += gridDim.x;
-      tiles.begin(a, q, (load_set * WAVES + wave) * NT);
+      load_tile += step;
+      tiles.begin(a, q, load_tile + own, end);
     }
   };
-  const auto add = [&](const Step<NT, GB>& step) {
+  const auto add = [&](const Step<NT, GB>& from) {
     const int staged = ONCE ? block : block % span;
     if (!ONCE && staged == 0) {
       __syncthreads();
@@ -411,18 +430,18 @@ __global__ __launch_bounds__(WAVES* kWave, kResident) void k_linear_q4(LinearQ4A
 #pragma unroll
       for (int t = 0; t < NT; t++) {
 #pragma unroll
-        for (int i = 0; i < GB; i++) word[t][i] = step.w[t][g * GB + i];
-        scale[t] = step.scale(t, g, whole);
+        for (int i = 0; i < GB; i++) word[t][i] = from.w[t][g * GB + i];
+        scale[t] = from.scale(t, g, whole);
       }
       add_group<T, MT, NT, GB>(frags, sums, staged + g * GB, word, scale, acc);
     }
     block += 4;
     if (block < q.blocks) return;
-    const int64_t tile = (set * WAVES + wave) * NT;
+    const int64_t tile = tile0 + own;
 #pragma unroll
     for (int t = 0; t < NT; t++) {
       const int64_t n = (tile + t) * 16 + r;
-      if (n < q.N) {
+      if (tile + t < end && n < q.N) {
 #pragma unroll
         for (int mt = 0; mt < MT; mt++)
 #pragma unroll
@@ -430,7 +449,7 @@ __global__ __launch_bounds__(WAVES* kWave, kResident) void k_linear_q4(LinearQ4A
             const int m = m0 + mt * 16 + (lane >> 4) * 4 + i;
             if (m >= a.M) continue;
             const int64_t at = m * a.ldy + n;
-            const float v = acc[t][mt][i] + step.bias[t];
+            const float v = acc[t][mt][i] + from.bias[t];
             if (a.out_dtype == W2V_DTYPE_F32) {
               store_as<float>(a.y, at, v);
             } else {
@@ -442,7 +461,7 @@ __global__ __launch_bounds__(WAVES* kWave, kResident) void k_linear_q4(LinearQ4A
       for (int mt = 0; mt < MT; mt++) acc[t][mt] = f32x4{};
     }
     block = 0;
-    set += gridDim.x;
+    tile0 += step;
   };
   Step<NT, GB> even, odd;
   load(even);
@@ -450,10 +469,10 @@ __global__ __launch_bounds__(WAVES* kWave, kResident) void k_linear_q4(LinearQ4A
     stage<T, MT, GB, WAVES, true>(a, q, m0, 0, q.blocks, frags, sums);
     __syncthreads();
   }
-  while (set < sets) {
+  while (tile0 < end) {
     load(odd);
     add(even);
-    if (set >= sets) break;
+    if (tile0 >= end) break;
     load(even);
     add(odd);
   }
@@ -497,7 +516,6 @@ hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, int span, hipStream_t
 // 37 us with four of 16.
 template <typename T, int MT, int GB>
 hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
-  constexpr int kAll = kResident * 4;
   const int most = most_blocks<T>(MT, GB * 32);
   if (q.blocks > most) return launch<T, MT, GB, kAll, false>(a, q, most, s);
   if (q.blocks * block_bytes<T>(MT, GB) <= kLds / kResident)
