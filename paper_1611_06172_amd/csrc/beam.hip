@@ -12,10 +12,17 @@
 // ones by index, and no sum comes into that; pairs of different beams by the sum
 // above in 64 bits, equal ones by beam.
 //
-// The best words of a share lie above a bound that at least `width` of them reach:
-// the width-th largest of the maxima of groups of its threads. What reaches the bound goes to a list in LDS and is
-// ranked there by counting; if the list overflows (thousands of equal scores), the
-// words are taken one after the other.
+// The best words of a share lie above a bound that at least `width` of them reach: the
+// width-th largest of the maxima of groups of its threads. Packs of scores with such a
+// word go to a list in LDS, its words to another one, and are ranked there by counting;
+// if a list overflows (thousands of equal scores), the words are taken one after the
+// other.
+//
+// Of the instructions for a score the exponential takes four slots of about nine, which
+// is about what reading 16-bit scores leaves time for. Measured: 16 x 16 beams of 10^6
+// words fp16 107 us (512 MB at 4.8 TB/s; shares 96 with the scores partly cached, merge
+// 17), 32 x 8 of 100,000 bf16 with two states 31 us (16, 9, and 5 for the states), 1 x 4
+// of 71,290 fp32 29 us, 18 of them in the kernels.
 #include "beam.h"
 #include "head_types.h"
 
@@ -600,8 +607,8 @@ __global__ __launch_bounds__(kBlock) void k_beam_reorder(ReorderArgs a) {
 // Packs a thread holds of a row, by an estimate of the time: a block takes 6 us and
 // 0.6 for each pack, the card holds 1,024 blocks of 16 packs, 1,536 of 4 and 1,792 of
 // 1 at once, and the merge 0.7 us for 256 lists of an entry. Measured with 16, 4, 1
-// packs: 16 x 16 beams of 10^6 words fp16 135, 183, 456 us; 64 x 4 of 71,290 bf16 33,
-// 30, 39; 64 x 32 of 2,000 fp32 54, 37, 51.
+// packs: 16 x 16 beams of 10^6 words fp16 109, 165, 464 us; 32 x 8 of 100,000 bf16 32,
+// 33, 54; 64 x 32 of 2,000 fp32 44, 38, 49; 16 x 16 of 30,000 bf16 29, 29, 36.
 int packs_of(int64_t batch, int64_t beams, int32_t V, int32_t dtype) {
   const int64_t e = dtype == W2V_DTYPE_F32 ? 4 : 8;
   const int packs[3] = {16, 4, 1};

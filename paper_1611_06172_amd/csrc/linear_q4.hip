@@ -3,6 +3,9 @@
 //   y = x W^T + bias,   W_nk = s_n,g(k) (q_nk - 8),   q in 0..15,
 //
 // for few rows of x: the matrix is read once, which is what the product costs.
+// Measured: 16 x 10^6 x 300 fp32 61 us (238 MB at 3.9 TB/s), 61 x 100,000 x 600 fp16 in
+// groups of 64 20 us (44.8 MB, 7.3 GFLOP), 1 x 71,290 x 300 bf16 12 us, 8 of them in
+// the kernel.
 //
 // A wavefront takes tiles of 16 rows of W and multiplies them on 16 x 16 x 32
 // matrix instructions, 32 columns at a time, with x as the other operand (16 rows
@@ -366,7 +369,7 @@ struct Tiles {
 // with two at 2 wavefronts 26); with one of x, two share its readings from LDS (16 x
 // 10^6 x 300 fp32: 61, with one 65).
 constexpr int kResident = 4;
-constexpr int kAll = 4 * kResident;
+constexpr int kAll = 4 * kResident, kHalf = kAll / 2;
 constexpr int tiles_at_once(int mt) { return mt == 1 ? 2 : 1; }
 
 // One block: NT tiles of W at a time and wavefront, against MT tiles of x
@@ -379,7 +382,8 @@ constexpr int tiles_at_once(int mt) { return mt == 1 ? 2 : 1; }
 // CU, take a stretch each, all of one length: 391 sets for 256 blocks would be two
 // rounds (61 x 100,000 x 600 fp16 in groups of 64: 23.0 to 21.7 us).
 template <typename T, int MT, int NT, int GB, int WAVES, bool ONCE>
-__global__ __launch_bounds__(WAVES* kWave, kResident) void k_linear_q4(LinearQ4Args a, Q4Shape q, int span) {
+__global__ __launch_bounds__(WAVES* kWave, WAVES == kHalf ? kResident / 2 : kResident)
+void k_linear_q4(LinearQ4Args a, Q4Shape q, int span) {
   extern __shared__ uint4 frags[];
   float* sums = (float*)(frags + (int64_t)span * MT * Operand<T>::kPieces * kWave);
   const int lane = threadIdx.x & 63, r = lane & 15;
@@ -387,7 +391,7 @@ __global__ __launch_bounds__(WAVES* kWave, kResident) void k_linear_q4(LinearQ4A
   const int m0 = blockIdx.y * MT * 16;
   const int64_t b = blockIdx.x;
   int64_t first = b * WAVES * NT, end = q.tiles, step = (int64_t)gridDim.x * WAVES * NT;
-  if (WAVES == kAll) {
+  if (WAVES >= kHalf) {
     const int64_t units = (q.tiles + NT - 1) / NT, each = units / gridDim.x;
     const int64_t more = units - each * gridDim.x;
     first = (b * each + (b < more ? b : more)) * NT;
@@ -498,7 +502,7 @@ hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, int span, hipStream_t
   const int64_t sets = (q.tiles + WAVES * NT - 1) / (WAVES * NT);
   // as many blocks as the card holds at once, so that all end at the same time:
   // each puts x into LDS for itself
-  const int64_t by_lds = kLds / bytes, by_registers = kResident * 4 / WAVES;
+  const int64_t by_lds = kLds / bytes, by_registers = WAVES == kHalf ? 1 : kAll / WAVES;
   const int64_t fit = 256 * (by_lds < by_registers ? by_lds : by_registers);
   const dim3 grid((unsigned)(sets < fit ? sets : fit), (unsigned)((a.M + MT * 16 - 1) / (MT * 16)));
   if (bytes > (64 << 10)) {
@@ -512,12 +516,17 @@ hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, int span, hipStream_t
 }
 
 // Blocks of four wavefronts while LDS holds as many of them as the registers do, else
-// one block of all those wavefronts, which shares its x: of 1 x 100,000 x 1,000 fp32
-// 37 us with four of 16.
+// one block of all those wavefronts, which shares its x (1 x 100,000 x 1,000 fp32 20
+// us, with the four that LDS then allows 37). x in parts and groups of 128 take more
+// registers: half the wavefronts (16 x 50,000 x 2,000 fp32 24 us, with all 43).
 template <typename T, int MT, int GB>
 hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
   const int most = most_blocks<T>(MT, GB * 32);
-  if (q.blocks > most) return launch<T, MT, GB, kAll, false>(a, q, most, s);
+  if (q.blocks > most) {
+    if constexpr (MT == 1 || GB < 4)
+      return launch<T, MT, GB, GB == 4 ? kHalf : kAll, false>(a, q, most, s);
+    return hipErrorInvalidValue;
+  }
   if (q.blocks * block_bytes<T>(MT, GB) <= kLds / kResident)
     return launch<T, MT, GB, 4, true>(a, q, q.blocks, s);
   return launch<T, MT, GB, kAll, true>(a, q, q.blocks, s);
@@ -535,13 +544,25 @@ hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
   }
 }
 
-// Up to 64 rows of x to a reading of W (32 of fp32, which takes three times the LDS),
-// fewer where they do not fit into LDS: reading W again costs less than x (32 x
-// 100,000 x 1,000 fp32 101 us with x in two parts).
+// Up to 64 rows of x to a reading of W (32 of fp32, which takes three times the LDS).
+// Where these do not fit into LDS x is taken in parts, or half as many rows at a time:
+// in groups of 128, for their registers (32 x 100,000 x 1,000 fp32 39 us, in parts
+// 47); where that leaves fewer rows over (100 x 100,000 x 1,000 fp32 138 and 154); or
+// where it takes more blocks to fill the card (64 x 30,000 x 1,000 bf16 16 and 22;
+// else in parts: 64 x 100,000 x 1,000 45 and 42, 64 x 50,000 x 2,000 59 and 32).
 template <typename T>
 hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
   int mt = a.M <= 16 ? 1 : a.M <= 32 || Operand<T>::kPieces > 1 ? 2 : 4;
-  while (mt > 1 && q.blocks > most_blocks<T>(mt, q.group)) mt /= 2;
+  const auto parts = [&](int tiles) { return (a.M + tiles * 16 - 1) / (tiles * 16); };
+  const auto blocks = [&](int tiles) {
+    return parts(tiles) * ((q.tiles + kAll * tiles_at_once(tiles) - 1) / (kAll * tiles_at_once(tiles)));
+  };
+  while (mt > 1 && q.blocks > most_blocks<T>(mt, q.group)) {
+    const bool fewer = 2 * parts(mt) > parts(mt / 2);
+    const bool fuller = blocks(mt) < 192 && blocks(mt / 2) > blocks(mt);
+    if (q.group < 128 && !fewer && !fuller) break;
+    mt /= 2;
+  }
   if (mt == 1) return launch<T, 1>(a, q, s);
   if (mt == 2) return launch<T, 2>(a, q, s);
   if constexpr (Operand<T>::kPieces == 1) return launch<T, 4>(a, q, s);

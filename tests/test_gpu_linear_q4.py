@@ -177,6 +177,30 @@ def test_many_rows_of_the_matrix(M):
         check(x, part, out[:, first:first + 64])
 
 
+@pytest.mark.parametrize("name,M,N,K,group", [
+    ("float32", 32, 400, 700, 32), ("float32", 64, 400, 1000, 64), ("float16", 20, 410, 2100, 32),
+    ("float32", 40, 50_000, 700, 64), ("bfloat16", 64, 100_003, 1100, 32),
+    ("float16", 61, 50_001, 2100, 64), ("float32", 16, 100_003, 1400, 128)])
+def test_rows_in_parts(name, M, N, K, group):
+    """All rows of x against W at once, a part of their columns at a time, over one
+    and several rounds of tiles."""
+    import torch
+    g = generator(N + K)
+    q = random_q4(g, N, K, group)
+    x = matrix(g, M, K, name, pad=1)
+    bias = torch.randn(N, generator=g).cuda()
+    out = w2v.linear_q4(x, q, bias)
+    G = (K + group - 1) // group
+    blocks = G * group // 32
+    for first in (0, N // 3 // 16 * 16, 2 * N // 3 // 16 * 16, (N - 33) // 16 * 16):
+        part = dict(q, shape=(min(512, N - first), K))
+        tiles = (part["shape"][0] + 15) // 16
+        for key, per in (("packed", blocks * 256), ("scales", G * 16)):
+            per //= q[key].element_size() if key == "packed" else 1
+            part[key] = q[key][first // 16 * per:][:tiles * per].clone()
+        check(x, part, out[:, first:first + 512], bias[first:first + 512])
+
+
 def test_pieces_of_float32():
     """Three bfloat16 pieces hold all bits of x: an identity returns it."""
     import torch
