@@ -310,8 +310,10 @@ int w2v_beam_reorder(const w2v_beam_state* states, int32_t count, const int32_t*
       return fail(W2V_EINVAL, "states: a row stride is out of range");
     if (batch > 0 && (s.src == nullptr || s.dst == nullptr))
       return fail(W2V_EINVAL, "states: src or dst is NULL");
-    if (batch > 0 && s.src == s.dst)
-      return fail(W2V_EINVAL, "states: rows cannot be reordered in place");
+    // also not by states that change places
+    for (int32_t j = 0; j < count && batch > 0; j++)
+      if (s.dst == states[j].src || (j != i && s.dst == states[j].dst))
+        return fail(W2V_EINVAL, "states: rows cannot be reordered in place");
     a.states[i] = s;
   }
   int32_t* status = nullptr;

@@ -140,6 +140,16 @@ def test_beam_batches_beyond_31_bits():
     assert w2v.lib().w2v_beam_step_workspace_bytes(2, 3, 3, 100, 0) % 256 == 0
 
 
+@pytest.mark.parametrize("places", [((0, 1), (1, 0)), ((0, 2), (1, 2)), ((0, 2), (1, 0))])
+def test_beam_reorder_rejects_states_that_change_places(places):
+    table = (w2v._BeamState * 2)(*(
+        w2v._BeamState(src=FAKE + 4096 * src, src_stride=8, dst=FAKE + 4096 * dst, dst_stride=8,
+                       row_bytes=8) for src, dst in places))
+    refused(w2v.lib().w2v_beam_reorder,
+            dict(states=table, count=2, parents=FAKE, batch=2, beams=3, width=3, stream=None),
+            "in place")
+
+
 @pytest.mark.parametrize("over,needle,code", [
     (dict(count=-1), "count", -1), (dict(count=17), "count", -1), (dict(states=None), "states", -1),
     (dict(parents=None), "parents", -1), (dict(beams=0), "beams", -1), (dict(width=65), "width", -1),
