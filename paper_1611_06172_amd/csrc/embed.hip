@@ -195,7 +195,8 @@ Clear clear_of(const EmbedBackwardArgs& a, int64_t first, int64_t last, int thre
     c.flat = c.n * (int64_t)c.row_bytes;
     blocks = (c.flat + 16 * threads - 1) / (16 * threads);
   }
-  c.blocks = (int32_t)(blocks < kMaxGrid ? blocks : kMaxGrid);
+  const int64_t most = kMaxGrid / (threads / kBlock);  // 2^30 threads; a launch takes 2^32
+  c.blocks = (int32_t)(blocks < most ? blocks : most);
   return c;
 }
 

@@ -68,6 +68,25 @@ def test_absent_words_read_nothing_of_their_own():
     assert w2v.embed(ids, w).tolist() == [[0.0] * 40, [2.0] * 40, [0.0] * 40]
 
 
+def test_gradient_of_more_chunks_than_a_launch_has_threads():
+    """72 GB cleared by blocks of 1,024 beside the sort: 4.5 x 10^9 chunks."""
+    import torch
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("needs 100 GiB of GPU memory")
+    V, D = 60_000_000, 300
+    grad = torch.ones((V, D), device="cuda")
+    ids = torch.tensor([V - 1, 5, 5, 31_234_567], dtype=torch.int32, device="cuda")
+    dy = torch.full((4, D), 2.0, device="cuda")
+    w2v.embed_backward(dy, ids, grad=grad)
+    for row, want in ((V - 1, 2.0), (5, 4.0), (31_234_567, 2.0)):
+        assert (grad[row] == want).all()
+        grad[row] = 0
+    for first in range(0, V, 1_000_000):
+        assert not grad[first:first + 1_000_000].any()
+    del grad
+    torch.cuda.empty_cache()
+
+
 def test_rows_beyond_32_bit_offsets():
     """Offsets past 2^32 elements in the matrix and past 2^31 bytes in y."""
     import torch
