@@ -14,9 +14,10 @@
 //
 // The best words of a share lie above a bound that at least `width` of them reach: the
 // width-th largest of the maxima of groups of its threads. Packs of scores with such a
-// word go to a list in LDS, its words to another one, and are ranked there by counting;
-// if a list overflows (thousands of equal scores), the words are taken one after the
-// other.
+// word go to a list in LDS, its words to another one, and are ranked there by counting.
+// Of too many words those above the bound are taken, and the first that equal it (32 x 8
+// beams of 100,000 words all alike 45 us, one after the other 105); if that is still more
+// than the list holds, one after the other.
 //
 // Of the instructions for a score the exponential takes four slots of about nine, which
 // is about what reading 16-bit scores leaves time for. Measured: 16 x 16 beams of 10^6
@@ -35,6 +36,7 @@ constexpr int kWaves = kBlock / kWave;
 constexpr int kMaxGrid = 1 << 22;
 constexpr int kList = 1024;
 constexpr int kPackList = 512;
+constexpr int kMany = 256;  // words that are ranked at once without a second look
 constexpr float kInf = __builtin_inff();
 
 __device__ __forceinline__ bool live_score(float c) { return c > -kInf; }  // not NaN
@@ -155,6 +157,17 @@ struct Row {
     asm volatile("" : "+v"(m));
     return m;
   }
+  // Which scores of pack p equal v, as bits.
+  __device__ __forceinline__ uint32_t equal(int p, float v) {
+    float z[kE];
+    repack(p);
+    unpack_words<T>(__builtin_bit_cast(uint4, w[p]), z);
+    uint32_t bits = 0;
+#pragma unroll
+    for (int e = 0; e < kE; e++) bits |= z[e] == v ? 1u << e : 0;
+    asm volatile("" : "+v"(bits));
+    return bits;
+  }
   // Sum of exp(z - top). Of fp16 exp2(z k - t), t the rounded top k, is one
   // instruction before the exponential, with the conversion, where exp2((z - top) k)
   // takes three; that sum is 2^(top k - t) times too large or small, at most
@@ -199,6 +212,51 @@ struct Row {
   }
 };
 
+// The next larger fp32 number of a finite one.
+__device__ __forceinline__ float next_above(float v) {
+  const int32_t bits = __builtin_bit_cast(int32_t, v);
+  if (v == 0.0f) return __builtin_bit_cast(float, 1);
+  return __builtin_bit_cast(float, bits + (bits < 0 ? -1 : 1));
+}
+
+// Puts the first `most` of a share's scores that equal v, by index, into a list.
+// Returns how many there are of them.
+template <typename T, int PACKS>
+__device__ __forceinline__ int take_equal(Row<T, PACKS>& z, float v, int most,
+                                          int (&of_waves)[kWaves], Word* list) {
+  constexpr int kE = Row<T, PACKS>::kE, kBits = PACKS * kE, kWords = (kBits + 31) / 32;
+  uint32_t mask[kWords] = {};
+#pragma unroll
+  for (int p = 0; p < PACKS; p++) mask[p * kE / 32] |= z.equal(p, v) << (p * kE % 32);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int total = 0;
+  for (int p = 0; p < PACKS && total < most; p++) {
+    uint32_t here = 0;
+#pragma unroll
+    for (int i = 0; i < kWords; i++)
+      if (p * kE / 32 == i) here = mask[i];
+    here = here >> (p * kE % 32) & ((1u << kE) - 1);
+    const int mine = __popc(here);
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const int below = __shfl_up(upto, d);
+      if (lane >= d) upto += below;
+    }
+    if (lane == kWave - 1) of_waves[wave] = upto;
+    __syncthreads();
+    int at = total + upto - mine;
+    for (int w = 0; w < kWaves; w++) {
+      if (w < wave) at += of_waves[w];
+      total += of_waves[w];
+    }
+    for (; here != 0 && at < most; here &= here - 1)
+      list[at++] = {v, (p * kBlock + (int)threadIdx.x) * kE + __builtin_ctz(here)};
+    __syncthreads();
+  }
+  return total < most ? total : most;
+}
+
 template <typename T, int PACKS>
 __global__ __launch_bounds__(kBlock, 4) void k_beam_shares(BeamArgs a, int shares, Share* out,
                                                         Word* best) {
@@ -208,6 +266,7 @@ __global__ __launch_bounds__(kBlock, 4) void k_beam_shares(BeamArgs a, int share
   __shared__ word4 s_pack[kPackList];
   __shared__ int s_first[kPackList];
   __shared__ Word s_list[kList];
+  __shared__ int s_equal[kWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   constexpr int kE = Row<T, PACKS>::kE;
   const int64_t units = (int64_t)a.batch * a.beams * shares;
@@ -242,31 +301,44 @@ __global__ __launch_bounds__(kBlock, 4) void k_beam_shares(BeamArgs a, int share
     if (lane == 0) s_wave[kWaves + wave] = sum;
     __syncthreads();
     // the packs that hold words to take, then those words; of a NaN neither
-    const float bound = fmaxf(s_bound.get(a.width), -__FLT_MAX__);
+    const auto take = [&](float from) {
 #pragma unroll
-    for (int p = 0; p < PACKS; p += kPer)
-      if (of_packs[p / kPer] >= bound) {
-        const int at = atomicAdd(&s_packs, kPer);
-        if (at <= kPackList - kPer) {
+      for (int p = 0; p < PACKS; p += kPer)
+        if (of_packs[p / kPer] >= from) {
+          const int at = atomicAdd(&s_packs, kPer);
+          if (at <= kPackList - kPer) {
 #pragma unroll
-          for (int u = 0; u < kPer; u++) {
-            s_pack[at + u] = z.w[p + u];
-            s_first[at + u] = ((p + u) * kBlock + (int)threadIdx.x) * kE;
+            for (int u = 0; u < kPer; u++) {
+              s_pack[at + u] = z.w[p + u];
+              s_first[at + u] = ((p + u) * kBlock + (int)threadIdx.x) * kE;
+            }
           }
         }
-      }
-    __syncthreads();
-    const int packs = s_packs;
-    if (packs <= kPackList)
-      for (int i = threadIdx.x; i < packs * kE; i += kBlock) {
-        const float v = to_f32(((const T*)s_pack)[i]);
-        if (v >= bound) {
-          const int at = atomicAdd(&s_count, 1);
-          if (at < kList) s_list[at] = {v, s_first[i / kE] + i % kE};
+      __syncthreads();
+      const int packs = s_packs;
+      if (packs <= kPackList)
+        for (int i = threadIdx.x; i < packs * kE; i += kBlock) {
+          const float v = to_f32(((const T*)s_pack)[i]);
+          if (v >= from) {
+            const int at = atomicAdd(&s_count, 1);
+            if (at < kList) s_list[at] = {v, s_first[i / kE] + i % kE};
+          }
         }
-      }
-    __syncthreads();
-    const int count = packs <= kPackList ? s_count : kList + 1;
+      __syncthreads();
+      return packs <= kPackList ? s_count : kList + 1;
+    };
+    const float bound = fmaxf(s_bound.get(a.width), -__FLT_MAX__);
+    int count = take(bound);
+    if (count > kMany) {
+      // what is more than the bound, and the first `width` of those that equal it: a
+      // model whose scores are all alike takes no longer
+      __syncthreads();
+      if (threadIdx.x == 0) s_packs = s_count = 0;
+      __syncthreads();
+      count = take(next_above(bound));
+      if (count < a.width)
+        count += take_equal(z, bound, a.width - count, s_equal, s_list + count);
+    }
     Word* to = best + unit * a.width;
     if (count <= kList) {
       for (int i = threadIdx.x; i < count; i += kBlock) {

@@ -201,6 +201,26 @@ def test_equal_scores(name, width, batch, beams, V):
 
 
 @pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("width", [1, 5, 16, 64])
+@pytest.mark.parametrize("level", [0.0, -2.5, "lowest"])
+def test_few_words_above_equal_ones(name, width, level):
+    """Some words above thousands that are alike, which come in order of the index."""
+    import torch
+    g = generator(8)
+    lowest = torch.finfo(dtype_of(name)).min
+    for batch, beams, V in ((1, 3, 900), (2, 2, 70_001), (40, 8, 30_000)):
+        z = torch.full((batch * beams, V), lowest if level == "lowest" else level,
+                       dtype=dtype_of(name))
+        z[:, :9] = float("-inf")
+        for row in z:
+            row[torch.randint(0, V, (7,), generator=g)] += 1.5
+            row[torch.randint(0, V, (5,), generator=g)] = -0.0
+        z = z.cuda()
+        scores = -torch.arange(float(beams)).expand(batch, -1).contiguous().cuda()
+        check(z, scores, w2v.beam_step(z, scores, width=width), width)
+
+
+@pytest.mark.parametrize("name", NAMES)
 @pytest.mark.parametrize("width", [16, 64])
 def test_best_words_in_few_threads(name, width):
     """Scores that rise towards one place, or that few of a share's threads hold:
