@@ -3,7 +3,7 @@
 //   y = x W^T + bias,   W_nk = s_n,g(k) (q_nk - 8),   q in 0..15,
 //
 // for few rows of x: the matrix is read once, which is what the product costs.
-// Measured: 16 x 10^6 x 300 fp32 61 us (238 MB at 3.9 TB/s), 61 x 100,000 x 600 fp16 in
+// Measured: 16 x 10^6 x 300 fp32 63 us (238 MB at 3.8 TB/s), 61 x 100,000 x 600 fp16 in
 // groups of 64 20 us (44.8 MB, 7.3 GFLOP), 1 x 71,290 x 300 bf16 12 us, 8 of them in
 // the kernel.
 //
@@ -21,7 +21,12 @@
 // The group's sum times its scale is added in fp32.
 //
 // fp32 x is taken apart into three bfloat16 pieces of 8 bits each, which hold all
-// of its 24 bits: three instructions for one, and nothing is rounded.
+// of its 24 bits: three instructions for one, and nothing is rounded. The correction of
+// the first pieces, whose sum takes few bits, is what the accumulator begins at; the
+// others', 2^-8 of it, is added behind the products. In one number it would be rounded
+// to 2^-24 of itself, and it is many times the sum (600 normal columns in groups of 32,
+// 128: errors of 6.1e-7 and 1.3e-6 of the result's size, so 1.1e-7 and 2.1e-7, a product
+// in fp32 4.0e-7; 16 x 10^6 x 300 60.5 us, so 63).
 #include "head_types.h"
 #include "linear_q4.h"
 
@@ -109,19 +114,19 @@ template <typename T>
 struct Operand {  // of fp32 x: pieces in bfloat16
   typedef bf16x8 Vec;
   typedef bf16_t Element;
-  static constexpr int kPieces = 3;
+  static constexpr int kPieces = 3, kSums = 2;  // the first pieces', the others'
 };
 template <>
 struct Operand<bf16_t> {
   typedef bf16x8 Vec;
   typedef bf16_t Element;
-  static constexpr int kPieces = 1;
+  static constexpr int kPieces = 1, kSums = 1;
 };
 template <>
 struct Operand<f16_t> {
   typedef f16x8 Vec;
   typedef f16_t Element;
-  static constexpr int kPieces = 1;
+  static constexpr int kPieces = 1, kSums = 1;
 };
 
 // 16 + q for the eight codes of a word.
@@ -161,7 +166,7 @@ __device__ __forceinline__ void store_as(void* y, int64_t at, float v) {
 
 // x in LDS as the instruction wants it, for `blocks` blocks of columns at a time:
 // [block][tile of rows][piece][lane] of 16 bytes, and behind these -24 sum(x) of
-// each group and row.
+// each group and row [group][tile of rows][kSums][row].
 // A wavefront takes kUnits groups of 16 rows at a time, whose loads are on their way
 // together (one between products, where the registers are taken); only the end of a
 // row is loaded with a test.
@@ -194,7 +199,7 @@ __device__ __forceinline__ void stage(const LinearQ4Args& a, const Q4Shape& q, i
     for (int i = 0; i < kUnits; i++) {
       const int u = u0 + i * WAVES, g = u / MT, mt = u % MT;
       if (u >= units) break;
-      float sum = 0.0f;
+      float sum = 0.0f, rest = 0.0f;
 #pragma unroll
       for (int b = 0; b < GB; b++) {
         Pack<T, 8> v = in[i][b];
@@ -216,12 +221,13 @@ __device__ __forceinline__ void stage(const LinearQ4Args& a, const Q4Shape& q, i
 #pragma unroll
           for (int j = 0; j < 8; j++) {
             float left = v.v[j];
-            sum += left;
 #pragma unroll
             for (int p = 0; p < 3; p++) {
               piece[p][j] = upper(left);
               left -= __builtin_bit_cast(float, piece[p][j] << 16);
+              if (p == 0) rest += left;
             }
+            sum += __builtin_bit_cast(float, piece[0][j] << 16);
           }
 #pragma unroll
           for (int p = 0; p < 3; p++) {
@@ -232,9 +238,15 @@ __device__ __forceinline__ void stage(const LinearQ4Args& a, const Q4Shape& q, i
           }
         }
       }
+      float* to = sums + (g * MT + mt) * Op::kSums * 16 + r;
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
-      if (quad == 0) sums[(g * MT + mt) * 16 + r] = -24.0f * sum;
+      if (quad == 0) to[0] = -24.0f * sum;
+      if constexpr (Op::kSums > 1) {
+        rest += __shfl_xor(rest, 16);
+        rest += __shfl_xor(rest, 32);
+        if (quad == 0) to[16] = -24.0f * rest;
+      }
     }
   }
 }
@@ -250,31 +262,43 @@ __device__ __forceinline__ void add_group(const uint4* frags, const float* sums,
   f32x4 part[NT][MT];
 #pragma unroll
   for (int mt = 0; mt < MT; mt++) {
-    const f32x4 first = *(const f32x4*)(sums + (block / GB * MT + mt) * 16 + (lane >> 4) * 4);
+    const f32x4 first =
+        *(const f32x4*)(sums + (block / GB * MT + mt) * Op::kSums * 16 + (lane >> 4) * 4);
 #pragma unroll
     for (int t = 0; t < NT; t++) part[t][mt] = first;
   }
+  // of fp32 x the first pieces of all blocks, then the others, so that what is rounded
+  // behind the first ones is small
 #pragma unroll
-  for (int b = 0; b < GB; b++) {
-    Vec w[NT];
+  for (int p0 = 0; p0 < Op::kSums; p0++)
 #pragma unroll
-    for (int t = 0; t < NT; t++) w[t] = codes_of<Vec>(word[t][b]);
+    for (int b = 0; b < GB; b++) {
+      Vec w[NT];
 #pragma unroll
-    for (int mt = 0; mt < MT; mt++)
+      for (int t = 0; t < NT; t++) w[t] = codes_of<Vec>(word[t][b]);
 #pragma unroll
-      for (int p = 0; p < Op::kPieces; p++) {
-        const Vec x = __builtin_bit_cast(
-            Vec, frags[(((block + b) * MT + mt) * Op::kPieces + p) * kWave + lane]);
+      for (int mt = 0; mt < MT; mt++)
 #pragma unroll
-        for (int t = 0; t < NT; t++) part[t][mt] = multiply(x, w[t], part[t][mt]);
+        for (int p = p0; p < (p0 == 0 ? 1 : Op::kPieces); p++) {
+          const Vec x = __builtin_bit_cast(
+              Vec, frags[(((block + b) * MT + mt) * Op::kPieces + p) * kWave + lane]);
+#pragma unroll
+          for (int t = 0; t < NT; t++) part[t][mt] = multiply(x, w[t], part[t][mt]);
+        }
+    }
+#pragma unroll
+  for (int mt = 0; mt < MT; mt++) {
+    f32x4 rest = {};
+    if constexpr (Op::kSums > 1)
+      rest = *(const f32x4*)(sums + (block / GB * MT + mt) * Op::kSums * 16 + 16 + (lane >> 4) * 4);
+#pragma unroll
+    for (int t = 0; t < NT; t++)
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const float sum = Op::kSums > 1 ? part[t][mt][i] + rest[i] : part[t][mt][i];
+        acc[t][mt][i] = fmaf(scale[t], sum, acc[t][mt][i]);
       }
   }
-#pragma unroll
-  for (int t = 0; t < NT; t++)
-#pragma unroll
-    for (int mt = 0; mt < MT; mt++)
-#pragma unroll
-      for (int i = 0; i < 4; i++) acc[t][mt][i] = fmaf(scale[t], part[t][mt][i], acc[t][mt][i]);
 }
 
 // Cache policy of the words, which are read once: they do not drive x and the scales
@@ -366,11 +390,14 @@ struct Tiles {
 
 // Wavefronts of a SIMD that the registers are to allow, 128 each. That takes one tile
 // of W at a time with several of x (61 x 100,000 x 600 fp16 in groups of 64: 23 us,
-// with two at 2 wavefronts 26); with one of x, two share its readings from LDS (16 x
-// 10^6 x 300 fp32: 61, with one 65).
+// with two at 2 wavefronts 26), and of fp32 x in groups of 128 (1 x 100,000 x 1,000 17
+// us, with two 22); else, with one of x, two share its readings from LDS (16 x 10^6 x
+// 300 fp32: 61, with one 65).
 constexpr int kResident = 4;
 constexpr int kAll = 4 * kResident, kHalf = kAll / 2;
-constexpr int tiles_at_once(int mt) { return mt == 1 ? 2 : 1; }
+constexpr int tiles_at_once(int mt, int pieces, int gb) {
+  return mt > 1 || (pieces > 1 && gb == 4) ? 1 : 2;
+}
 
 // One block: NT tiles of W at a time and wavefront, against MT tiles of x
 // (blockIdx.y). `span` blocks of columns of x are in LDS at once; where that is all of
@@ -378,7 +405,7 @@ constexpr int tiles_at_once(int mt) { return mt == 1 ? 2 : 1; }
 // A wavefront goes through the steps of all its tiles with the next one's loads on
 // their way.
 // Small blocks take sets of neighbouring tiles in turn: W is read in its order (16 x
-// 10^6 x 300 fp32 61 us, each block with a stretch of its own 64). Large ones, one a
+// 10^6 x 300 fp32 3 us less than with a stretch for each block). Large ones, one a
 // CU, take a stretch each, all of one length: 391 sets for 256 blocks would be two
 // rounds (61 x 100,000 x 600 fp16 in groups of 64: 23.0 to 21.7 us).
 template <typename T, int MT, int NT, int GB, int WAVES, bool ONCE>
@@ -487,7 +514,7 @@ constexpr int kMostLds = 128 << 10, kLds = 160 << 10;
 // LDS of a block of columns of x.
 template <typename T>
 constexpr int block_bytes(int mt, int gb) {
-  return mt * Operand<T>::kPieces * kWave * 16 + mt * 16 * 4 / gb;
+  return mt * Operand<T>::kPieces * kWave * 16 + mt * Operand<T>::kSums * 16 * 4 / gb;
 }
 // Blocks of columns of x that LDS holds.
 template <typename T>
@@ -497,7 +524,7 @@ int most_blocks(int mt, int group) {
 
 template <typename T, int MT, int GB, int WAVES, bool ONCE>
 hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, int span, hipStream_t s) {
-  constexpr int NT = tiles_at_once(MT);
+  constexpr int NT = tiles_at_once(MT, Operand<T>::kPieces, GB);
   const int bytes = span * block_bytes<T>(MT, GB);
   const int64_t sets = (q.tiles + WAVES * NT - 1) / (WAVES * NT);
   // as many blocks as the card holds at once, so that all end at the same time:
@@ -555,7 +582,8 @@ hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
   int mt = a.M <= 16 ? 1 : a.M <= 32 || Operand<T>::kPieces > 1 ? 2 : 4;
   const auto parts = [&](int tiles) { return (a.M + tiles * 16 - 1) / (tiles * 16); };
   const auto blocks = [&](int tiles) {
-    return parts(tiles) * ((q.tiles + kAll * tiles_at_once(tiles) - 1) / (kAll * tiles_at_once(tiles)));
+    const int64_t of = kAll * tiles_at_once(tiles, Operand<T>::kPieces, q.group / 32);
+    return parts(tiles) * ((q.tiles + of - 1) / of);
   };
   while (mt > 1 && q.blocks > most_blocks<T>(mt, q.group)) {
     const bool fewer = 2 * parts(mt) > parts(mt / 2);

@@ -201,6 +201,29 @@ def test_rows_in_parts(name, M, N, K, group):
         check(x, part, out[:, first:first + 512], bias[first:first + 512])
 
 
+@pytest.mark.parametrize("M", [1, 20])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_correction_is_not_rounded(M, group):
+    """x of 16 bits in [1, 2), scales of 2^-3: in multiples of 2^-15, 24 sum(x) takes more
+    than 24 bits, but the result fewer, and those of its first pieces, and so does every
+    sum on the way as it is documented: nothing is rounded."""
+    import torch
+    g = generator(group)
+    K, N = 2 * group, 200
+    w = torch.randint(-7, 8, (N, K), generator=g).float()
+    w[:, ::group] = 7.0
+    x = 1.0 + torch.randint(0, 1 << 15, (M, K), generator=g).float() / (1 << 15)
+    want = x.double() @ (w.double() / 8).t()
+    fits = want.abs() < 32  # with 31 |x| 2^-7 of the others' products: 9 bits before the point
+    for half in (w[:, :group], w[:, group:]):
+        fits &= (x[:, :group].double() @ half.double().t()).abs() < 256
+        fits &= (x[:, group:].double() @ half.double().t()).abs() < 256
+    assert fits.float().mean() > 0.5
+    q = w2v.quantize_q4((w / 8).cuda(), group=group)
+    y = w2v.linear_q4(x.cuda(), q).cpu().double()
+    assert torch.equal(y[fits], want[fits])
+
+
 def test_pieces_of_float32():
     """Three bfloat16 pieces hold all bits of x: an identity returns it."""
     import torch
