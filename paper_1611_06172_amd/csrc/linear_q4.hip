@@ -4,7 +4,7 @@
 //
 // for few rows of x: the matrix is read once, which is what the product costs.
 // Measured: 16 x 10^6 x 300 fp32 63 us (238 MB at 3.8 TB/s), 61 x 100,000 x 600 fp16 in
-// groups of 64 20 us (44.8 MB, 7.3 GFLOP), 1 x 71,290 x 300 bf16 12 us, 8 of them in
+// groups of 64 19 to 21 us (44.8 MB, 7.3 GFLOP), 1 x 71,290 x 300 bf16 12 us, 8 of them in
 // the kernel.
 //
 // A wavefront takes tiles of 16 rows of W and multiplies them on 16 x 16 x 32
