@@ -390,6 +390,16 @@ __device__ __forceinline__ bool better(const Pair& a, const Pair& b) {
   return (a.key > b.key) | ((a.key == b.key) & beam);
 }
 
+__device__ __forceinline__ Pair best_of_wave(Pair p) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    const Pair o = {__shfl_xor(p.key, d), __shfl_xor(p.z, d), __shfl_xor(p.beam, d),
+                    __shfl_xor(p.id, d)};
+    if (better(o, p)) p = o;
+  }
+  return p;
+}
+
 __global__ __launch_bounds__(kBlock) void k_beam_merge(BeamArgs a, int shares, const Share* share,
                                                        const Word* best) {
   __shared__ double s_add[W2V_MAX_BEAMS];     // what a beam's scores are added to
@@ -478,7 +488,8 @@ __global__ __launch_bounds__(kBlock) void k_beam_merge(BeamArgs a, int shares, c
     };
     double first = -(double)kInf;
     if (way < ways && way < a.width)
-      for (int list = list0; list < lists; list += kBlock) first = fmax(first, pair_of(list, way).key);
+      for (int list = list0; list < lists; list += kBlock)
+        first = fmax(first, pair_of(list, way).key);
     // in fp32: rounding keeps the keys' order, so no pair above the bound is lost
     s_bound.begin((float)first, a.width);
     __syncthreads();
@@ -590,31 +601,40 @@ __global__ __launch_bounds__(kBlock) void k_beam_merge(BeamArgs a, int shares, c
       }
       for (int i = count + threadIdx.x; i < a.width; i += kBlock) write(i, none, false);
     } else {
-      // one after the other: of each list the first pair behind the last taken
+      // one after the other: of each list the first pair behind the last taken, from
+      // where a thread found it before in its first kHeld lists
+      constexpr int kHeld = 4;
       Pair last = {(double)kInf, 0.0f, 0, 0};
+      int next[kHeld];
+#pragma unroll
+      for (int u = 0; u < kHeld; u++) next[u] = way;
       for (int n = 0; n < a.width; n++) {
         Pair mine = none;
-        if (way < ways)
-          for (int list = list0; list < lists; list += kBlock)
-            for (int place = way; place < a.width; place += ways) {
-              const Pair p = pair_of(list, place);
-              if (!(p.key > -(double)kInf)) break;
-              if (!better(last, p)) continue;
-              if (better(p, mine)) mine = p;
-              break;
-            }
-        __syncthreads();
-        s_list[threadIdx.x] = mine;
-        __syncthreads();
-        if (wave == 0) {
-          for (int w = 1; w < kWaves; w++)
-            if (better(s_list[w * kWave + lane], mine)) mine = s_list[w * kWave + lane];
-          s_list[lane] = mine;
+        const auto look = [&](int list, int& from) {
+          for (; from < a.width; from += ways) {
+            const Pair p = pair_of(list, from);
+            if (!(p.key > -(double)kInf)) break;
+            if (!better(last, p)) continue;
+            if (better(p, mine)) mine = p;
+            break;
+          }
+        };
+        if (way < ways) {
+#pragma unroll
+          for (int u = 0; u < kHeld; u++)
+            if (list0 + u * kBlock < lists) look(list0 + u * kBlock, next[u]);
+          for (int list = list0 + kHeld * kBlock; list < lists; list += kBlock) {
+            int from = way;
+            look(list, from);
+          }
         }
+        mine = best_of_wave(mine);
+        __syncthreads();
+        if (lane == 0) s_list[wave] = mine;
         __syncthreads();
         last = s_list[0];
-        for (int i = 1; i < kWave; i++)
-          if (better(s_list[i], last)) last = s_list[i];
+        for (int w = 1; w < kWaves; w++)
+          if (better(s_list[w], last)) last = s_list[w];
         if (threadIdx.x == 0) write(n, last, last.key > -(double)kInf);
       }
     }
@@ -654,7 +674,8 @@ __global__ __launch_bounds__(kBlock) void k_beam_reorder(ReorderArgs a) {
       const int32_t parent = a.parents[row];
       there[u] = parent >= 0 && parent < a.beams;
       if (!there[u] && parent != -1) report_row(a.status);
-      from[u] = (const char*)st.src + (entry * a.beams + (there[u] ? parent : 0)) * st.src_stride + at;
+      from[u] =
+          (const char*)st.src + (entry * a.beams + (there[u] ? parent : 0)) * st.src_stride + at;
       to[u] = some ? (char*)st.dst + row * st.dst_stride + at : nullptr;
     }
     if (whole) {

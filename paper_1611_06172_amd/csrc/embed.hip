@@ -27,7 +27,7 @@ namespace {
 
 constexpr int kE = 8;             // elements a lane takes of a row
 constexpr int kBlock = 256;
-constexpr int kPacks = 2;         // packs a thread has in flight (1: 220 us, 4: 207, where 2 take 204)
+constexpr int kPacks = 2;  // packs a thread has in flight (1: 220 us, 4: 207, where 2 take 204)
 constexpr int kBlockPacks = kPacks * kBlock;
 constexpr int kMaxGrid = 1 << 22;
 constexpr int kWave = 64;
@@ -320,7 +320,9 @@ struct SortPass {
   __device__ __forceinline__ uint32_t key(int64_t i) const {
     return ids != nullptr ? word_key(ids[i], V, status) : keys[i];
   }
-  __device__ __forceinline__ int digit(uint32_t k) const { return (int)(k >> shift) & (digits - 1); }
+  __device__ __forceinline__ int digit(uint32_t k) const {
+    return (int)(k >> shift) & (digits - 1);
+  }
 };
 
 __global__ __launch_bounds__(kBlock) void k_embed_count(SortPass p, int32_t* hist, Clear clear) {
@@ -758,7 +760,8 @@ __global__ __launch_bounds__(kBlock) void k_embed_spans(EmbedBackwardArgs a, Col
   add_rows<SHORT>(head + (int64_t)blockIdx.x * kSpan * cols.ld + l.first, cols.ld, kSpan,
                   threadIdx.x >> 6, kWaves, l.left, sum);
   join_waves(s_sum, sum);
-  if (threadIdx.x < kWave && l.there) put<SHORT>(spans + blockIdx.x * cols.ld + l.first, l.left, sum);
+  if (threadIdx.x < kWave && l.there)
+    put<SHORT>(spans + blockIdx.x * cols.ld + l.first, l.left, sum);
 }
 
 // Joins the partial sums of the words that go over their chunk's end and began in
@@ -812,7 +815,8 @@ __global__ __launch_bounds__(kBlock) void k_embed_join(EmbedBackwardArgs a, Colu
       // a span with the word's last chunk, which it may not fill, has no sum
       int64_t g0 = (from + kSpan - 1) / kSpan, g1 = (to - 1) / kSpan;
       if (spans == nullptr || g1 <= g0) g0 = g1 = to / kSpan + 1;
-      const int64_t stop = g0 * kSpan < to ? g0 * kSpan : to, on = g1 * kSpan < to ? g1 * kSpan : to;
+      const int64_t stop = g0 * kSpan < to ? g0 * kSpan : to;
+      const int64_t on = g1 * kSpan < to ? g1 * kSpan : to;
       Pack<float, kE> sum{};
       if (wave == 0) sum = get<SHORT>(tail + own_chunk * cols.ld + l.first, l.left);
       add_rows<SHORT>(head + from * cols.ld + l.first, cols.ld, (int)(stop - from), wave, kWaves,

@@ -183,7 +183,8 @@ def test_a_step_after_the_other():
 
 @pytest.mark.parametrize("name", NAMES)
 @pytest.mark.parametrize("width", [1, 8, 16, 17, 64])
-@pytest.mark.parametrize("batch,beams,V", [(2, 4, 900), (1, 3, 60_000), (40, 8, 40_000)])
+@pytest.mark.parametrize("batch,beams,V", [(2, 4, 900), (1, 3, 60_000), (40, 8, 40_000),
+                                           (1, 64, 300_000)])
 def test_equal_scores(name, width, batch, beams, V):
     """An untrained model: all words alike. The first ones of the best beam are
     taken, then the next beam's."""
