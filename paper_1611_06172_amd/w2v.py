@@ -997,9 +997,12 @@ def linear_q4(x, weight, bias=None, *, out_dtype=None, out=None, stream=None):
     N, group = weight["shape"][0], weight["group"]
     if weight["shape"][1] != K:
         raise ValueError("x and weight must have the same number of columns")
-    _vector(weight["packed"], torch.uint8, "packed", int(lib().w2v_q4_packed_bytes(N, K, group)))
-    _vector(weight["scales"], torch.bfloat16, "scales",
-            int(lib().w2v_q4_scale_count(N, K, group)))
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    # w2v_q4_packed_bytes and w2v_q4_scale_count, without the calls
+    tiles, groups = (N + 15) // 16, (K + group - 1) // group
+    _vector(weight["packed"], torch.uint8, "packed", tiles * groups * group * 8)
+    _vector(weight["scales"], torch.bfloat16, "scales", tiles * groups * 16)
     if bias is not None:
         _vector(bias, torch.float32, "bias", N)
     if out is not None:

@@ -181,3 +181,13 @@ def test_binding_rejects():
                  lambda: w2v.beam_reorder(w, ids.view(1, 3))):
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_sizes_of_a_matrix_in_4_bits(group):
+    """What the binding expects of a dict's arrays without asking the library."""
+    for N in (1, 16, 17, 71_290):
+        for K in (1, 31, 33, 300, 1000):
+            tiles, groups = (N + 15) // 16, (K + group - 1) // group
+            assert w2v.lib().w2v_q4_packed_bytes(N, K, group) == tiles * groups * group * 8
+            assert w2v.lib().w2v_q4_scale_count(N, K, group) == tiles * groups * 16
