@@ -305,7 +305,7 @@ __device__ __forceinline__ void add_group(const uint4* frags, const float* sums,
 // out (1 x 10^6 x 300: 57 to 52 us).
 constexpr int kNonTemporal = 2;
 
-// Range-checked access to `bytes` bytes: loads past them are 0.
+// Range-checked access to `bytes` bytes: loads whose lane's offset is past them are 0.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t checked(const void* p, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc((void*)p, (short)0, bytes, 0x00020000);
 }
@@ -343,47 +343,41 @@ struct Tiles {
 
   __device__ __forceinline__ void begin(const LinearQ4Args& a, const Q4Shape& q, int64_t tile,
                                         int64_t end) {
-    const int64_t left = end - tile;
-    const int count = left >= NT ? NT : left > 0 ? (int)left : 0;
-    const int64_t rows = q.N - tile * 16;
-    words = checked(a.packed + tile * q.blocks * 64, count * q.blocks * 256);
-    scales = checked((const bf16_t*)a.scales + tile * q.groups * 16, count * q.groups * 32);
-    bias = checked(a.bias + tile * 16,
-                   a.bias == nullptr || rows <= 0 ? 0 : (rows < NT * 16 ? (int)rows : NT * 16) * 4);
+    const Q4Range range = q4_range(q, tile, end, NT, a.bias != nullptr);
+    words = checked(a.packed + tile * q.blocks * 64, range.words);
+    scales = checked((const bf16_t*)a.scales + tile * q.groups * 16, range.scales);
+    bias = checked(a.bias + tile * 16, range.bias);
   }
   __device__ __forceinline__ void load(const Q4Shape& q, int block, Step<NT, GB>& step) const {
     const int lane = threadIdx.x & 63, r = lane & 15;
-    const int rest = q.blocks - block;
-    const int group = block / GB, first = group & ~3;
+    const int rest = q.blocks - block, group = block / GB;
     const bool whole = whole_scales<GB>(q, block);
     step = Step<NT, GB>{};  // nothing of the step before is kept alive
 #pragma unroll
     for (int t = 0; t < NT; t++) {
-      const int from = (t * q.blocks + block) * 256;
+      const int from = q4_words_at(q, t, block, lane);
       if (rest >= 4) {
-        step.w[t] = __builtin_amdgcn_raw_buffer_load_b128(words, lane * 16, from, kNonTemporal);
+        step.w[t] = __builtin_amdgcn_raw_buffer_load_b128(words, from, 0, kNonTemporal);
       } else {
-        const int at = lane * rest * 4;
-        step.w[t].x = __builtin_amdgcn_raw_buffer_load_b32(words, at, from, 0);
-        step.w[t].y = __builtin_amdgcn_raw_buffer_load_b32(words, at + 4, from, 0);
-        step.w[t].z = __builtin_amdgcn_raw_buffer_load_b32(words, at + 8, from, 0);
+        step.w[t].x = __builtin_amdgcn_raw_buffer_load_b32(words, from, 0, 0);
+        step.w[t].y = __builtin_amdgcn_raw_buffer_load_b32(words, from + 4, 0, 0);
+        step.w[t].z = __builtin_amdgcn_raw_buffer_load_b32(words, from + 8, 0, 0);
       }
-      const int row = t * q.groups * 32 + first * 32 + (group - first) * 2;
+      const int at = q4_scales_at(q, t, group, r);
       if (GB == 1 && whole) {
-        const auto four = __builtin_amdgcn_raw_buffer_load_b64(scales, r * 8, row, 0);
+        const auto four = __builtin_amdgcn_raw_buffer_load_b64(scales, at, 0, 0);
         step.four[t][0] = four[0];
         step.four[t][1] = four[1];
       } else {
-        const int at = whole ? r * 8 : r * (q.groups - first) * 2;
 #pragma unroll
         for (int g = 0; g < Step<NT, GB>::kSingle; g++)
-          step.single[t][g] = __builtin_amdgcn_raw_buffer_load_b16(scales, at + 2 * g, row, 0);
+          step.single[t][g] = __builtin_amdgcn_raw_buffer_load_b16(scales, at + 2 * g, 0, 0);
       }
       // in time for the step that ends the tile; with larger groups a test costs more
       // than the load (61 x 100,000 x 600 in groups of 64: 31 to 29 us)
       if (GB > 1 || rest <= 4)
         step.bias[t] = __builtin_bit_cast(
-            float, __builtin_amdgcn_raw_buffer_load_b32(bias, r * 4, t * 64, 0));
+            float, __builtin_amdgcn_raw_buffer_load_b32(bias, q4_bias_at(t, r), 0, 0));
     }
   }
 };
