@@ -309,17 +309,17 @@ constexpr int kTileGroups = 8;  // of a wavefront
 constexpr int kTileWaves = kBlock / kWave;
 constexpr int kTile = kTileWaves * kTileGroups * kWave;  // 2,048
 
-// A pass's keys: words (the first pass) or the pass before's.
+// A pass's keys: words, which the first pass's counting copies, or the pass before's.
+// Words are read that once: whatever becomes of them meanwhile, the counts are those of
+// the keys that are sent, so that every place is taken, once.
 struct SortPass {
   const int32_t* ids;  // or NULL
+  uint32_t* copy;      // of their keys
   const uint32_t* keys;
-  const int32_t* at;
+  const int32_t* at;  // or NULL: where they are
   int32_t n, V, shift, digits, tiles;
   int32_t* status;
 
-  __device__ __forceinline__ uint32_t key(int64_t i) const {
-    return ids != nullptr ? word_key(ids[i], V, status) : keys[i];
-  }
   __device__ __forceinline__ int digit(uint32_t k) const {
     return (int)(k >> shift) & (digits - 1);
   }
@@ -335,8 +335,11 @@ __global__ __launch_bounds__(kBlock) void k_embed_count(SortPass p, int32_t* his
   const int64_t first = (int64_t)blockIdx.x * kTile + threadIdx.x;
   uint32_t key[kTileGroups];
 #pragma unroll
-  for (int g = 0; g < kTileGroups; g++)
-    key[g] = first + g * kBlock < p.n ? p.key(first + g * kBlock) : 0;
+  for (int g = 0; g < kTileGroups; g++) {
+    const int64_t i = first + g * kBlock;
+    key[g] = i >= p.n ? 0 : p.ids != nullptr ? word_key(p.ids[i], p.V, p.status) : p.keys[i];
+    if (p.ids != nullptr && i < p.n) p.copy[i] = key[g];
+  }
   __syncthreads();
 #pragma unroll
   for (int g = 0; g < kTileGroups; g++)
@@ -435,8 +438,8 @@ __global__ __launch_bounds__(kBlock) void k_embed_scatter(SortPass p, const int3
 #pragma unroll
   for (int g = 0; g < kTileGroups; g++) {
     const int64_t i = first + g * kWave;
-    key[g] = i < p.n ? p.key(i) : 0;
-    from[g] = i < p.n ? (p.ids != nullptr ? (int32_t)i : p.at[i]) : 0;
+    key[g] = i < p.n ? p.keys[i] : 0;
+    from[g] = i < p.n ? (p.at == nullptr ? (int32_t)i : p.at[i]) : 0;
   }
   __syncthreads();
 #pragma unroll
@@ -495,8 +498,9 @@ __global__ __launch_bounds__(kBlock) void k_embed_scatter(SortPass p, const int3
     const uint64_t same = lanes_with(set, d) & __ballot(there);
     const int rank = __popcll(same & lanes_below(lane));
     const int place = s_next[wave][d] + rank;
-    // places lie in [0, n) by construction; the test keeps a fault out of reach
-    // should the tables ever disagree
+    // places lie in [0, n) by construction. Should a workspace be written by another
+    // call all the same, the test here and that of the sums' rows (row_in) keep what
+    // is done within the arguments
     if (there && place >= 0 && place < p.n) {
       keys[place] = key[g];
       at[place] = from[g];
@@ -529,6 +533,11 @@ __device__ __forceinline__ LaneColumns lane_columns(const Columns& c, int32_t D,
   l.skip = l.there ? pack * kE - l.first : 0;
   l.left = D - l.first;
   return l;
+}
+
+// A row of dy from the sorted list.
+__device__ __forceinline__ int32_t row_in(int32_t at, int32_t n) {
+  return (uint32_t)at < (uint32_t)n ? at : 0;
 }
 
 // One word's finished sum. Of a pack that begins early only the lane's own
@@ -583,7 +592,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_sums(EmbedBackwardArgs a, Colu
   const LaneColumns l = lane_columns<false>(cols, a.D, (int)threadIdx.x & 63);
   const uint32_t V = (uint32_t)a.V;
   const uint32_t key = lane < size ? keys[begin + lane] : V;
-  const int32_t row = lane < size ? at[begin + lane] : 0;
+  const int32_t row = lane < size ? row_in(at[begin + lane], a.n) : 0;
   const uint32_t before = begin > 0 ? keys[begin - 1] : ~0u;
   const uint32_t after = begin + size < a.n ? keys[begin + size] : ~0u;
   // words only: absent ones come last
@@ -660,7 +669,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_team_sums(EmbedBackwardArgs a,
     Pack<TI, kE> in[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; u++)
-      in[u] = get_once<SHORT>(dy + (j0 + u < size ? row.v[u] : 0) * a.lddy, l.left);
+      in[u] = get_once<SHORT>(dy + (j0 + u < size ? row_in(row.v[u], a.n) : 0) * a.lddy, l.left);
     const int64_t from = j0 + kAhead < size ? begin + j0 + kAhead : begin;
     next_key = load_pack<uint32_t, kAhead>(keys + from);
     next_row = load_pack<int32_t, kAhead>(at + from);
@@ -959,6 +968,7 @@ void launch_order(const EmbedBackwardArgs& a, const Workspace& w, hipStream_t s)
     const bool to_out = (passes - 1 - pass) % 2 == 0;
     uint32_t* keys = to_out ? w.sorted : w.keys;
     int32_t* at = to_out ? w.at : w.at_before;
+    p.copy = to_out ? w.keys : w.sorted;  // of the two, the one that the pass does not write
     Clear c = clear_next();
     hipLaunchKernelGGL(k_embed_count, dim3(p.tiles + c.blocks), dim3(kBlock), 0, s, p, w.hist, c);
     if (p.tiles > kFewTiles) {
@@ -966,10 +976,11 @@ void launch_order(const EmbedBackwardArgs& a, const Workspace& w, hipStream_t s)
       hipLaunchKernelGGL(k_embed_scan, dim3((p.digits + kWave - 1) / kWave + c.blocks),
                          dim3(kScanWaves * kWave), 0, s, p, w.hist, w.totals, c);
     }
+    if (p.ids != nullptr) p.keys = p.copy;
+    p.ids = nullptr;
     c = clear_next();
     hipLaunchKernelGGL(k_embed_scatter, dim3(p.tiles + c.blocks), dim3(kBlock), 0, s, p, w.hist,
                        w.totals, keys, at, c);
-    p.ids = nullptr;
     p.keys = keys;
     p.at = at;
   }

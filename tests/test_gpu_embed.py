@@ -315,3 +315,31 @@ def test_refused_arguments():
                  lambda: w2v.embed_backward(w[:3], ids, grad=torch.zeros((5, 9), device="cuda"))):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("n,V", [(20_000, 700), (20_000, 5_000), (300_000, 5_000),
+                                 (300_000, 2_000_000)])
+def test_words_that_change_during_the_call(n, V):
+    """Every row is added to one of the words that stood in its place, once, whatever
+    another stream writes there meanwhile: the sums are of whole numbers below 2^24, so
+    nothing is rounded."""
+    import torch
+    g = generator(n + V)
+    a = torch.randint(0, V, (n,), generator=g, dtype=torch.int32).cuda()
+    b = (V - 1 - a).contiguous()
+    dy = torch.randint(-3, 4, (n, 8), generator=g).float().cuda()
+    want = dy.double().sum(0)
+    ids = a.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(10):
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                ids.copy_(b)
+                ids.copy_(a)
+        grad = w2v.embed_backward(dy, ids, V)
+        assert torch.equal(grad.double().sum(0), want)
+    side.synchronize()
+    check = torch.zeros((V, 8), dtype=torch.float64, device="cuda")
+    check.index_add_(0, a.long(), dy.double())
+    assert torch.equal(w2v.embed_backward(dy, ids, V).double(), check)
