@@ -725,10 +725,10 @@ int w2v_quantize_q4(const void* w, int64_t ldw, int32_t N, int32_t K, int32_t dt
  * y = x W^T + bias for such a W, x M x K of `dtype` and y M x N of `out_dtype`
  * (dtype or W2V_DTYPE_F32); bias: device float[N] or NULL. Made for few rows:
  * the matrix is read once for every 64 of them (16-bit x) or 32 (fp32), or for
- * fewer with K in the hundreds or more. Products are exact and sums fp32: of a group, sum x (q + 16) - 24 sum x, so x whose
- * magnitudes add up to more than 2^122 in a group may overflow, and a row of x
- * with an infinity gives NaN. Each output is rounded once; the same call gives
- * the same bits. M = 0 is allowed and does nothing; M <= W2V_MAX_Q4_ROWS. y must
+ * fewer with K in the thousands. Products x (q - 8) are exact and sums fp32: a
+ * group's, which is multiplied with its scale, and the row's. A row of x with an
+ * infinity gives NaN. Each output is rounded once; the same call gives the same
+ * bits. M = 0 is allowed and does nothing; M <= W2V_MAX_Q4_ROWS. y must
  * not overlap any other argument.
  */
 #define W2V_MAX_Q4_ROWS 524288

@@ -4,7 +4,7 @@
 //
 // for few rows of x: the matrix is read once, which is what the product costs.
 // Measured: 16 x 10^6 x 300 fp32 63 us (238 MB at 3.8 TB/s), 61 x 100,000 x 600 fp16 in
-// groups of 64 19 to 21 us (44.8 MB, 7.3 GFLOP), 1 x 71,290 x 300 bf16 12 us, 8 of them in
+// groups of 64 20 to 21 us (44.8 MB, 7.3 GFLOP), 1 x 71,290 x 300 bf16 12 us, 8 of them in
 // the kernel.
 //
 // A wavefront takes tiles of 16 rows of W and multiplies them on 16 x 16 x 32
@@ -13,20 +13,18 @@
 // of a wavefront finds the eight codes of row r that the instruction wants from it
 // in one word, the words of four blocks of columns in 16 bytes.
 //
-// A code becomes a 16-bit float by a shift and one and-or: 16 + q is 2^4 (1 + q /
-// 16), whose fraction's upper bits are q. The product with x is thus 24 sum(x) too
-// large in every group; the accumulator begins at minus that. The products are
-// exact and are summed in fp32, and so is the correction, which makes the rounding
-// error of a group that of sums of 31 |x| instead of 8 |x|, still 2^-24 of them.
-// The group's sum times its scale is added in fp32.
+// What is multiplied is q - 8, which both 16-bit types hold, so that products are exact
+// and a group's sum is rounded as one of fp32 numbers is, in whatever order the
+// instruction takes them. (Codes of 16 + q, a shift and an and-or, with a correction of
+// -24 sum(x) are 7 instructions fewer a word of bfloat16 and 4 of fp16, but their sums
+// are tens of times the result where x has a mean. 384 columns of mean 1 in groups of
+// 128: errors of 1.9e-6, 1.9e-6 and 4.3e-6 of the result's size with fp32, bf16 and fp16
+// x, so 1.2e-7, 3.6e-8 and 3.9e-8, a product in fp32 3.2e-7, 9e-8 and 2.2e-7. 16 x 10^6 x
+// 300 fp32 62 us both ways, bf16 48, so 52.) The group's sum times its scale is added in
+// fp32.
 //
 // fp32 x is taken apart into three bfloat16 pieces of 8 bits each, which hold all
-// of its 24 bits: three instructions for one, and nothing is rounded. The correction of
-// the first pieces, whose sum takes few bits, is what the accumulator begins at; the
-// others', 2^-8 of it, is added behind the products. In one number it would be rounded
-// to 2^-24 of itself, and it is many times the sum (600 normal columns in groups of 32,
-// 128: errors of 6.1e-7 and 1.3e-6 of the result's size, so 1.1e-7 and 2.1e-7, a product
-// in fp32 4.0e-7; 16 x 10^6 x 300 60.5 us, so 63).
+// of its 24 bits: three instructions for one, and nothing is rounded.
 #include "head_types.h"
 #include "linear_q4.h"
 
@@ -114,37 +112,56 @@ template <typename T>
 struct Operand {  // of fp32 x: pieces in bfloat16
   typedef bf16x8 Vec;
   typedef bf16_t Element;
-  static constexpr int kPieces = 3, kSums = 2;  // the first pieces', the others'
+  static constexpr int kPieces = 3;
 };
 template <>
 struct Operand<bf16_t> {
   typedef bf16x8 Vec;
   typedef bf16_t Element;
-  static constexpr int kPieces = 1, kSums = 1;
+  static constexpr int kPieces = 1;
 };
 template <>
 struct Operand<f16_t> {
   typedef f16x8 Vec;
   typedef f16_t Element;
-  static constexpr int kPieces = 1, kSums = 1;
+  static constexpr int kPieces = 1;
 };
 
-// 16 + q for the eight codes of a word.
+// e4m3 of the codes less 8 in the bytes of q, each 0 to 15. A byte selection takes one
+// of eight bytes for 0 to 7, and for 8 to 15 zeros, ones or the sign of a byte, which are
+// known. So one looks up the negative numbers and one, by q ^ 8, the others; each table
+// is taken exclusive-or with what the other selection gives there.
+__device__ __forceinline__ uint32_t numbers_of(uint32_t q) {
+  const uint32_t negative = __builtin_amdgcn_perm(0x473F3BC8u, 0x3533CED0u, q);
+  const uint32_t others = __builtin_amdgcn_perm(0xB1B3B548u, 0x444038FFu, q ^ 0x08080808u);
+  return negative ^ others;
+}
+
+// q - 8 for the eight codes of a word: of bfloat16 in the order 0, 4, 1, 5, 2, 6, 3, 7
+// of the columns. fp16: 16 + q is 2^4 (1 + q / 16), whose fraction's upper bits are q.
 template <typename Vec>
 __device__ __forceinline__ Vec codes_of(uint32_t u) {
-  uint4 w;
   if constexpr (__is_same(Vec, f16x8)) {
+    uint4 w;
     w.x = (u << 6 & 0x03C003C0u) | 0x4C004C00u;
     w.y = (u << 2 & 0x03C003C0u) | 0x4C004C00u;
     w.z = (u >> 2 & 0x03C003C0u) | 0x4C004C00u;
     w.w = (u >> 6 & 0x03C003C0u) | 0x4C004C00u;
+    return __builtin_bit_cast(Vec, w) - (f16_t)24.0f;
   } else {
-    w.x = (u << 3 & 0x00780078u) | 0x41804180u;
-    w.y = (u >> 1 & 0x00780078u) | 0x41804180u;
-    w.z = (u >> 5 & 0x00780078u) | 0x41804180u;
-    w.w = (u >> 9 & 0x00780078u) | 0x41804180u;
+    const uint32_t low = numbers_of(u & 0x0F0F0F0Fu), high = numbers_of(u >> 4 & 0x0F0F0F0Fu);
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(low, 1.0f, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(low, 1.0f, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(high, 1.0f, false);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(high, 1.0f, true);
+    return Vec{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
   }
-  return __builtin_bit_cast(Vec, w);
+}
+// Which of eight columns is in a place of the operands.
+template <typename T>
+__device__ __forceinline__ constexpr int column_at(int place) {
+  return __is_same(T, f16_t) ? place : place / 2 + place % 2 * 4;
 }
 
 __device__ __forceinline__ f32x4 multiply(bf16x8 a, bf16x8 b, f32x4 c) {
@@ -164,88 +181,90 @@ __device__ __forceinline__ void store_as(void* y, int64_t at, float v) {
   ((T*)y)[at] = from_f32<T>(v);
 }
 
+// Eight 16-bit x, with a NaN among them if there is an infinity: the row becomes NaN
+// whatever codes it meets. Products with 0 find it, two in an instruction. (The pieces of
+// an infinite fp32 x are that and inf - inf.)
+template <typename T>
+__device__ __forceinline__ uint4 not_infinite(uint4 x) {
+  typedef T Two __attribute__((ext_vector_type(2)));
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  float zero = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    if constexpr (__is_same(T, f16_t)) {
+      zero = __builtin_amdgcn_fdot2(__builtin_bit_cast(Two, w[i]), Two{}, zero, false);
+    } else {
+      zero = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(Two, w[i]), Two{}, zero, false);
+    }
+  }
+  if (zero != zero) x.x |= 0x7FFFu;
+  return x;
+}
+
 // x in LDS as the instruction wants it, for `blocks` blocks of columns at a time:
-// [block][tile of rows][piece][lane] of 16 bytes, and behind these -24 sum(x) of
-// each group and row [group][tile of rows][kSums][row].
-// A wavefront takes kUnits groups of 16 rows at a time, whose loads are on their way
-// together (one between products, where the registers are taken); only the end of a
+// [block][tile of rows][piece][lane] of 16 bytes.
+// A wavefront takes kUnits blocks of 16 rows at a time, whose loads are on their way
+// together (fewer between products, where the registers are taken); only the end of a
 // row is loaded with a test.
 template <typename T, int MT, int GB, int WAVES, bool ONCE>
 __device__ __forceinline__ void stage(const LinearQ4Args& a, const Q4Shape& q, int m0, int b0,
-                                      int blocks, uint4* frags, float* sums) {
+                                      int blocks, uint4* frags) {
   typedef Operand<T> Op;
-  constexpr int kUnits = ONCE ? 4 / GB : 1;
+  constexpr int kUnits = ONCE ? 4 : GB;
   const int lane = threadIdx.x & 63, r = lane & 15, quad = lane >> 4;
-  const int units = blocks / GB * MT;
+  const int units = blocks * MT;
   const T* x = (const T*)a.x;
   for (int u0 = threadIdx.x >> 6; u0 < units; u0 += WAVES * kUnits) {
-    Pack<T, 8> in[kUnits][GB];
-    int64_t from[kUnits][GB];
-    int there[kUnits][GB];
+    Pack<T, 8> in[kUnits];
+    int64_t from[kUnits];
+    int there[kUnits];
 #pragma unroll
     for (int i = 0; i < kUnits; i++) {
-      const int u = u0 + i * WAVES, g = u / MT, m = m0 + u % MT * 16 + r;
-#pragma unroll
-      for (int b = 0; b < GB; b++) {
-        const int64_t k = ((int64_t)b0 + g * GB + b) * 32 + quad * 8;
-        const bool some = u < units && m < a.M && k < q.K;
-        there[i][b] = !some ? 0 : q.K - k < 8 ? (int)(q.K - k) : 8;
-        from[i][b] = some ? m * a.ldx + k : 0;
-        if (q.K >= 8) in[i][b] = load_pack<T, 8>(x + (there[i][b] == 8 ? from[i][b] : 0));
-      }
+      const int u = u0 + i * WAVES, m = m0 + u % MT * 16 + r;
+      const int64_t k = ((int64_t)b0 + u / MT) * 32 + quad * 8;
+      const bool some = u < units && m < a.M && k < q.K;
+      there[i] = !some ? 0 : q.K - k < 8 ? (int)(q.K - k) : 8;
+      from[i] = some ? m * a.ldx + k : 0;
+      if (q.K >= 8) in[i] = load_pack<T, 8>(x + (there[i] == 8 ? from[i] : 0));
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < kUnits; i++) {
-      const int u = u0 + i * WAVES, g = u / MT, mt = u % MT;
+      const int u = u0 + i * WAVES;
       if (u >= units) break;
-      float sum = 0.0f, rest = 0.0f;
-#pragma unroll
-      for (int b = 0; b < GB; b++) {
-        Pack<T, 8> v = in[i][b];
-        if (there[i][b] < 8) {
-          if (there[i][b] > 0) {
-            v = load_some<T, 8>(x + from[i][b], there[i][b]);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 8; j++) v.v[j] = T(0.0f);
-          }
-        }
-        uint4* to = frags + (((g * GB + b) * MT + mt) * Op::kPieces) * kWave + lane;
-        if constexpr (Op::kPieces == 1) {
-          to[0] = __builtin_bit_cast(uint4, v);
-#pragma unroll
-          for (int j = 0; j < 8; j++) sum += to_f32(v.v[j]);
+      Pack<T, 8> v = in[i];
+      if (there[i] < 8) {
+        if (there[i] > 0) {
+          v = load_some<T, 8>(x + from[i], there[i]);
         } else {
-          uint32_t piece[3][8];
 #pragma unroll
-          for (int j = 0; j < 8; j++) {
-            float left = v.v[j];
-#pragma unroll
-            for (int p = 0; p < 3; p++) {
-              piece[p][j] = upper(left);
-              left -= __builtin_bit_cast(float, piece[p][j] << 16);
-              if (p == 0) rest += left;
-            }
-            sum += __builtin_bit_cast(float, piece[0][j] << 16);
-          }
-#pragma unroll
-          for (int p = 0; p < 3; p++) {
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; j++) w[j] = piece[p][2 * j] | piece[p][2 * j + 1] << 16;
-            to[p * kWave] = make_uint4(w[0], w[1], w[2], w[3]);
-          }
+          for (int j = 0; j < 8; j++) v.v[j] = T(0.0f);
         }
       }
-      float* to = sums + (g * MT + mt) * Op::kSums * 16 + r;
-      sum += __shfl_xor(sum, 16);
-      sum += __shfl_xor(sum, 32);
-      if (quad == 0) to[0] = -24.0f * sum;
-      if constexpr (Op::kSums > 1) {
-        rest += __shfl_xor(rest, 16);
-        rest += __shfl_xor(rest, 32);
-        if (quad == 0) to[16] = -24.0f * rest;
+      uint4* to = frags + (int64_t)u * Op::kPieces * kWave + lane;
+      if constexpr (Op::kPieces == 1) {
+        Pack<T, 8> placed;
+#pragma unroll
+        for (int j = 0; j < 8; j++) placed.v[j] = v.v[column_at<T>(j)];
+        to[0] = not_infinite<T>(__builtin_bit_cast(uint4, placed));
+      } else {
+        uint32_t piece[3][8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          float left = v.v[column_at<T>(j)];
+#pragma unroll
+          for (int p = 0; p < 3; p++) {
+            piece[p][j] = upper(left);
+            left -= __builtin_bit_cast(float, piece[p][j] << 16);
+          }
+        }
+#pragma unroll
+        for (int p = 0; p < 3; p++) {
+          uint32_t w[4];
+#pragma unroll
+          for (int j = 0; j < 4; j++) w[j] = piece[p][2 * j] | piece[p][2 * j + 1] << 16;
+          to[p * kWave] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
       }
     }
   }
@@ -253,52 +272,34 @@ __device__ __forceinline__ void stage(const LinearQ4Args& a, const Q4Shape& q, i
 
 // GB blocks of a group: the words of NT tiles against MT tiles of x.
 template <typename T, int MT, int NT, int GB>
-__device__ __forceinline__ void add_group(const uint4* frags, const float* sums, int block,
+__device__ __forceinline__ void add_group(const uint4* frags, int block,
                                           const uint32_t (&word)[NT][GB], const float (&scale)[NT],
                                           f32x4 (&acc)[NT][MT]) {
   typedef Operand<T> Op;
   typedef typename Op::Vec Vec;
   const int lane = threadIdx.x & 63;
-  f32x4 part[NT][MT];
+  f32x4 part[NT][MT] = {};
 #pragma unroll
-  for (int mt = 0; mt < MT; mt++) {
-    const f32x4 first =
-        *(const f32x4*)(sums + (block / GB * MT + mt) * Op::kSums * 16 + (lane >> 4) * 4);
+  for (int b = 0; b < GB; b++) {
+    Vec w[NT];
 #pragma unroll
-    for (int t = 0; t < NT; t++) part[t][mt] = first;
+    for (int t = 0; t < NT; t++) w[t] = codes_of<Vec>(word[t][b]);
+#pragma unroll
+    for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+      for (int p = 0; p < Op::kPieces; p++) {
+        const Vec x = __builtin_bit_cast(
+            Vec, frags[(((block + b) * MT + mt) * Op::kPieces + p) * kWave + lane]);
+#pragma unroll
+        for (int t = 0; t < NT; t++) part[t][mt] = multiply(x, w[t], part[t][mt]);
+      }
   }
-  // of fp32 x the first pieces of all blocks, then the others, so that what is rounded
-  // behind the first ones is small
 #pragma unroll
-  for (int p0 = 0; p0 < Op::kSums; p0++)
-#pragma unroll
-    for (int b = 0; b < GB; b++) {
-      Vec w[NT];
-#pragma unroll
-      for (int t = 0; t < NT; t++) w[t] = codes_of<Vec>(word[t][b]);
-#pragma unroll
-      for (int mt = 0; mt < MT; mt++)
-#pragma unroll
-        for (int p = p0; p < (p0 == 0 ? 1 : Op::kPieces); p++) {
-          const Vec x = __builtin_bit_cast(
-              Vec, frags[(((block + b) * MT + mt) * Op::kPieces + p) * kWave + lane]);
-#pragma unroll
-          for (int t = 0; t < NT; t++) part[t][mt] = multiply(x, w[t], part[t][mt]);
-        }
-    }
-#pragma unroll
-  for (int mt = 0; mt < MT; mt++) {
-    f32x4 rest = {};
-    if constexpr (Op::kSums > 1)
-      rest = *(const f32x4*)(sums + (block / GB * MT + mt) * Op::kSums * 16 + 16 + (lane >> 4) * 4);
+  for (int mt = 0; mt < MT; mt++)
 #pragma unroll
     for (int t = 0; t < NT; t++)
 #pragma unroll
-      for (int i = 0; i < 4; i++) {
-        const float sum = Op::kSums > 1 ? part[t][mt][i] + rest[i] : part[t][mt][i];
-        acc[t][mt][i] = fmaf(scale[t], sum, acc[t][mt][i]);
-      }
-  }
+      for (int i = 0; i < 4; i++) acc[t][mt][i] = fmaf(scale[t], part[t][mt][i], acc[t][mt][i]);
 }
 
 // Cache policy of the words, which are read once: they do not drive x and the scales
@@ -406,7 +407,6 @@ template <typename T, int MT, int NT, int GB, int WAVES, bool ONCE>
 __global__ __launch_bounds__(WAVES* kWave, WAVES == kHalf ? kResident / 2 : kResident)
 void k_linear_q4(LinearQ4Args a, Q4Shape q, int span) {
   extern __shared__ uint4 frags[];
-  float* sums = (float*)(frags + (int64_t)span * MT * Operand<T>::kPieces * kWave);
   const int lane = threadIdx.x & 63, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m0 = blockIdx.y * MT * 16;
@@ -443,7 +443,7 @@ void k_linear_q4(LinearQ4Args a, Q4Shape q, int span) {
     if (!ONCE && staged == 0) {
       __syncthreads();
       stage<T, MT, GB, WAVES, false>(a, q, m0, block, q.blocks - block < span ? q.blocks - block : span,
-                                     frags, sums);
+                                     frags);
       __syncthreads();
     }
     const bool whole = whole_scales<GB>(q, block);
@@ -458,7 +458,7 @@ void k_linear_q4(LinearQ4Args a, Q4Shape q, int span) {
         for (int i = 0; i < GB; i++) word[t][i] = from.w[t][g * GB + i];
         scale[t] = from.scale(t, g, whole);
       }
-      add_group<T, MT, NT, GB>(frags, sums, staged + g * GB, word, scale, acc);
+      add_group<T, MT, NT, GB>(frags, staged + g * GB, word, scale, acc);
     }
     block += 4;
     if (block < q.blocks) return;
@@ -491,7 +491,7 @@ void k_linear_q4(LinearQ4Args a, Q4Shape q, int span) {
   Step<NT, GB> even, odd;
   load(even);
   if (ONCE) {
-    stage<T, MT, GB, WAVES, true>(a, q, m0, 0, q.blocks, frags, sums);
+    stage<T, MT, GB, WAVES, true>(a, q, m0, 0, q.blocks, frags);
     __syncthreads();
   }
   while (tile0 < end) {
@@ -507,19 +507,19 @@ constexpr int kMostLds = 128 << 10, kLds = 160 << 10;
 
 // LDS of a block of columns of x.
 template <typename T>
-constexpr int block_bytes(int mt, int gb) {
-  return mt * Operand<T>::kPieces * kWave * 16 + mt * Operand<T>::kSums * 16 * 4 / gb;
+constexpr int block_bytes(int mt) {
+  return mt * Operand<T>::kPieces * kWave * 16;
 }
 // Blocks of columns of x that LDS holds.
 template <typename T>
-int most_blocks(int mt, int group) {
-  return kMostLds / block_bytes<T>(mt, group / 32) & ~3;
+constexpr int most_blocks(int mt) {
+  return kMostLds / block_bytes<T>(mt) & ~3;
 }
 
 template <typename T, int MT, int GB, int WAVES, bool ONCE>
 hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, int span, hipStream_t s) {
   constexpr int NT = tiles_at_once(MT, Operand<T>::kPieces, GB);
-  const int bytes = span * block_bytes<T>(MT, GB);
+  const int bytes = span * block_bytes<T>(MT);
   const int64_t sets = (q.tiles + WAVES * NT - 1) / (WAVES * NT);
   // as many blocks as the card holds at once, so that all end at the same time:
   // each puts x into LDS for itself
@@ -536,19 +536,20 @@ hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, int span, hipStream_t
   return hipGetLastError();
 }
 
-// Blocks of four wavefronts while LDS holds as many of them as the registers do, else
-// one block of all those wavefronts, which shares its x (1 x 100,000 x 1,000 fp32 20
-// us, with the four that LDS then allows 37). x in parts and groups of 128 take more
-// registers: half the wavefronts (16 x 50,000 x 2,000 fp32 24 us, with all 43).
+// Blocks of four wavefronts while LDS holds as many of them as the registers do and has
+// room left, else one block of all those wavefronts, which shares its x (1 x 100,000 x
+// 1,000 fp32 20 us, with the four that LDS then allows 37; 64 x 100,000 x 300 bf16 15,
+// with four that fill it 19). x in parts and groups of 128 take more registers: half the
+// wavefronts (16 x 50,000 x 2,000 fp32 24 us, with all 43).
 template <typename T, int MT, int GB>
 hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
-  const int most = most_blocks<T>(MT, GB * 32);
+  const int most = most_blocks<T>(MT);
   if (q.blocks > most) {
     if constexpr (MT == 1 || GB < 4)
       return launch<T, MT, GB, GB == 4 ? kHalf : kAll, false>(a, q, most, s);
     return hipErrorInvalidValue;
   }
-  if (q.blocks * block_bytes<T>(MT, GB) <= kLds / kResident)
+  if (q.blocks * block_bytes<T>(MT) < kLds / kResident)
     return launch<T, MT, GB, 4, true>(a, q, q.blocks, s);
   return launch<T, MT, GB, kAll, true>(a, q, q.blocks, s);
 }
@@ -568,9 +569,10 @@ hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
 // Up to 64 rows of x to a reading of W (32 of fp32, which takes three times the LDS).
 // Where these do not fit into LDS x is taken in parts, or half as many rows at a time:
 // in groups of 128, for their registers (32 x 100,000 x 1,000 fp32 39 us, in parts
-// 47); where that leaves fewer rows over (100 x 100,000 x 1,000 fp32 138 and 154); or
-// where it takes more blocks to fill the card (64 x 30,000 x 1,000 bf16 16 and 22;
-// else in parts: 64 x 100,000 x 1,000 45 and 42, 64 x 50,000 x 2,000 59 and 32).
+// 47); where that leaves fewer rows over (90 x 71,290 x 2,000 bf16 103 and 122); or
+// where it takes more blocks to fill the card (64 x 30,000 x 1,100 bf16 16 and 21;
+// else in parts: 64 x 100,000 x 1,100 47 and 41, 64 x 50,000 x 2,000 fp16 in groups of
+// 64 39 and 30).
 template <typename T>
 hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
   int mt = a.M <= 16 ? 1 : a.M <= 32 || Operand<T>::kPieces > 1 ? 2 : 4;
@@ -579,7 +581,7 @@ hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, hipStream_t s) {
     const int64_t of = kAll * tiles_at_once(tiles, Operand<T>::kPieces, q.group / 32);
     return parts(tiles) * ((q.tiles + of - 1) / of);
   };
-  while (mt > 1 && q.blocks > most_blocks<T>(mt, q.group)) {
+  while (mt > 1 && q.blocks > most_blocks<T>(mt)) {
     const bool fewer = 2 * parts(mt) > parts(mt / 2);
     const bool fuller = blocks(mt) < 192 && blocks(mt / 2) > blocks(mt);
     if (q.group < 128 && !fewer && !fuller) break;
