@@ -584,6 +584,10 @@ def _head_dtype(t, name):
     return code
 
 
+# Sizes are 32-bit numbers of the library's; ctypes would pass on the lower bits of others.
+_MOST = 0x7FFFFFFF
+
+
 def _operand(t, name, shape=None, dtype=None):
     """Row stride of a 2-D GPU matrix whose columns are adjacent."""
     import torch
@@ -598,6 +602,8 @@ def _operand(t, name, shape=None, dtype=None):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(size)}")
     _here(t, name)
     rows, cols = size
+    if rows > _MOST or cols > _MOST:
+        raise ValueError(f"{name} must have less than 2^31 rows and columns")
     ld, step = t.stride()
     if cols > 1 and step != 1:
         raise ValueError(f"{name} must have unit column stride")
@@ -1126,6 +1132,8 @@ def beam_reorder(states, parents, *, out=None, stream=None):
             of = size[0] // batch if batch else 1
             if of * batch != size[0] or of < 1 or (beams is not None and of != beams):
                 raise ValueError("states must have batch * beams rows each")
+            if of > _MOST:
+                raise ValueError("states must have less than 2^31 rows of an entry")
             beams = of
             moved = (batch * width, *size[1:])
             if new is None:
