@@ -1090,6 +1090,8 @@ def _state_rows(t, name):
     size = t.shape
     if len(size) < 1:
         raise ValueError(f"{name} must have a first dimension")
+    if t.is_conj() or t.is_neg():
+        raise ValueError(f"{name} must hold its own values (resolve_conj, resolve_neg)")
     row = t.element_size()
     for n in size[1:]:
         row *= n

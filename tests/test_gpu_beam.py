@@ -457,3 +457,18 @@ def test_refused_arguments():
                  lambda: w2v.beam_reorder(z, parents, out=z)):
         with pytest.raises(w2v.W2VError):
             call()
+
+
+def test_states_that_stand_for_other_values_are_refused():
+    """Bytes are moved: those of a lazily conjugated or negated tensor are not its
+    values."""
+    import torch
+    parents = torch.tensor([[1, 0]], dtype=torch.int32, device="cuda")
+    z = torch.view_as_complex(torch.arange(12.0, device="cuda").view(2, 3, 2))
+    assert torch.equal(w2v.beam_reorder(z, parents), z.flip(0))
+    for lazy in (z.conj(), torch._neg_view(z.real.contiguous())):
+        with pytest.raises(ValueError, match="own values"):
+            w2v.beam_reorder(lazy, parents)
+        with pytest.raises(ValueError, match="own values"):
+            w2v.beam_reorder(torch.empty_like(lazy).copy_(lazy), parents, out=lazy)
+    assert torch.equal(w2v.beam_reorder(z.conj().resolve_conj(), parents), z.flip(0).conj())
