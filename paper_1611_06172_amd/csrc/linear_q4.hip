@@ -527,8 +527,9 @@ hipError_t launch(const LinearQ4Args& a, const Q4Shape& q, int span, hipStream_t
   const int64_t fit = 256 * (by_lds < by_registers ? by_lds : by_registers);
   const dim3 grid((unsigned)(sets < fit ? sets : fit), (unsigned)((a.M + MT * 16 - 1) / (MT * 16)));
   if (bytes > (64 << 10)) {
+    // the most of any call, since another thread's may lie between this and the launch
     const hipError_t e = hipFuncSetAttribute((const void*)k_linear_q4<T, MT, NT, GB, WAVES, ONCE>,
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, kMostLds);
     if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL((k_linear_q4<T, MT, NT, GB, WAVES, ONCE>), grid, dim3(WAVES * kWave), bytes,

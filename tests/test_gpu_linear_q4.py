@@ -323,3 +323,42 @@ def test_refused_arguments():
     for call in (lambda: w2v.quantize_q4(w, group=48), lambda: w2v.quantize_q4(w[:0])):
         with pytest.raises(w2v.W2VError):
             call()
+
+
+def test_calls_of_two_threads():
+    """Calls of one kernel with more and with less LDS, side by side."""
+    import threading
+
+    import torch
+    g = generator(12)
+    jobs, done = [], []
+    for K in (1000, 600):
+        q, x = random_q4(g, 200, K, 32), matrix(g, 60, K, "float16")
+        jobs.append((q, x, w2v.linear_q4(x, q)))
+
+    def work(q, x, want):
+        s = torch.cuda.Stream()
+        out = [w2v.linear_q4(x, q, stream=s) for _ in range(200)]
+        s.synchronize()
+        done.append(all(torch.equal(o, want) for o in out))
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=job) for job in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    assert done == [True, True]
+
+
+def test_much_of_lds_in_a_graph():
+    import torch
+    g = generator(13)
+    q, x = random_q4(g, 200, 1000, 32), matrix(g, 60, 1000, "float16")
+    graph, held = captured(lambda: w2v.linear_q4(x, q))
+    for _ in range(3):
+        x.copy_(torch.randn(x.shape, generator=g))
+        eager = w2v.linear_q4(x, q)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held, eager)
