@@ -643,7 +643,9 @@ int w2v_sample_words(const void* logits, int64_t ld, const float* uniforms, int6
  * the paper, which ends with the trained vectors.)
  *
  * Rows by word: y_i = scale W[id_i], for W V x D of `dtype` (M_in of a trained
- * model) and y n x D of `out_dtype`, any of the types, rounded once.
+ * model) and y n x D of `out_dtype`, any of the types. The product is one of fp32
+ * numbers, rounded as such and then, where scale is not a power of two, again to a
+ * 16-bit out_dtype.
  *   ids       device int32[n]: words; -1 = absent, whose row of y is 0. Any
  *             other id outside [0, V) gives a row of 0 too and is recorded in
  *             the device's error word.
@@ -661,8 +663,9 @@ int w2v_embed(const int32_t* ids, int32_t n, const void* weight, int64_t ldw, in
  *   negative scale makes it a step of gradient descent on the weight itself).
  * grad is V x D of `grad_dtype`, any of the types. Ids as in w2v_embed; absent
  * and out-of-range ones add nothing. Sums are held in fp32, over the positions
- * sorted by word, in an order that depends on the ids alone, and each element is
- * rounded once: the same call gives the same bits. workspace: device, 256-byte
+ * sorted by word, in an order that depends on the ids alone: the same call gives the
+ * same bits. The sum times scale (and the old value, in one fused operation) is rounded
+ * to fp32 and then to a 16-bit grad_dtype. Ids are read once. workspace: device, 256-byte
  * aligned, at least w2v_embed_backward_workspace_bytes(n, V, D) bytes (0 for n =
  * 0), contents need not be initialised; calls that overlap in time must not
  * share it. grad must not overlap any other argument.
@@ -688,8 +691,9 @@ int w2v_embed_backward(const void* dy, int64_t lddy, const int32_t* ids, int32_t
  *              caller counts it up;
  *   residual   or NULL (0); y may be x or the residual itself (same stride) and
  *              must not overlap them otherwise.
- * Whatever a dropped element holds (NaN, infinities) does not reach y. The
- * product and the sum are rounded once, as one. p = 0 keeps and p = 1 drops
+ * Whatever a dropped element holds (NaN, infinities) does not reach y. The factor
+ * 2^32 / (2^32 - B) is the nearest fp32 number; the product and the sum are formed in
+ * fp32, rounded as one, and then to a 16-bit dtype. p = 0 keeps and p = 1 drops
  * everything. Limits: 0 <= p <= 1, rows >= 0, 1 <= cols <= 2^30.
  */
 int w2v_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, void* y,
@@ -727,9 +731,8 @@ int w2v_quantize_q4(const void* w, int64_t ldw, int32_t N, int32_t K, int32_t dt
  * the matrix is read once for every 64 of them (16-bit x) or 32 (fp32), or for
  * fewer with K in the thousands. Products x (q - 8) are exact and sums fp32: a
  * group's, which is multiplied with its scale, and the row's. A row of x with an
- * infinity gives NaN. Each output is rounded once; the same call gives the same
- * bits. M = 0 is allowed and does nothing; M <= W2V_MAX_Q4_ROWS. y must
- * not overlap any other argument.
+ * infinity gives NaN. The same call gives the same bits. M = 0 is allowed and does
+ * nothing; M <= W2V_MAX_Q4_ROWS. y must not overlap any other argument.
  */
 #define W2V_MAX_Q4_ROWS 524288
 

@@ -191,3 +191,12 @@ def test_sizes_of_a_matrix_in_4_bits(group):
             tiles, groups = (N + 15) // 16, (K + group - 1) // group
             assert w2v.lib().w2v_q4_packed_bytes(N, K, group) == tiles * groups * group * 8
             assert w2v.lib().w2v_q4_scale_count(N, K, group) == tiles * groups * 16
+
+
+def test_most_rows_of_a_4_bit_product():
+    """W2V_MAX_Q4_ROWS is 524,288, in the header and in the check."""
+    args = dict(x=FAKE, ldx=8, packed=FAKE, scales=FAKE, bias=None, y=FAKE, ldy=5, M=524_289, N=5,
+                K=8, group=32, dtype=0, out=0, stream=None)
+    refused(w2v.lib().w2v_linear_q4, args, "M must be at most 524288", w2v.EUNSUPPORTED)
+    # as many as that pass it: the next check is another argument's
+    refused(w2v.lib().w2v_linear_q4, dict(args, M=524_288, x=None), "x is NULL")
