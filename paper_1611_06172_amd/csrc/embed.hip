@@ -7,7 +7,7 @@
 // Both move bytes and compute next to nothing: the lookup reads each different
 // row once (again from the caches) and writes n rows; the gradient reads n rows
 // and writes V, or reads and writes those that occur. Measured: 10^6 rows of 300 from
-// 10^6, fp32 to bf16, 202 us (795 MB at 3.9 TB/s); their gradient, bf16 to fp32, 441 us
+// 10^6, fp32 to bf16, 202 us (795 MB at 3.9 TB/s); their gradient, bf16 to fp32, 444 us
 // (1.8 GB at 4.1 TB/s: sort and clearing 240, sums 171, joins 17); 4,096 rows of 300
 // fp32 into 71,290, 26 us (91 MB at 3.5 TB/s); a lookup of 64 rows 9 us, 2.4 of them in
 // the kernel.

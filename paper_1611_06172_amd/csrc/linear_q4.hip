@@ -3,7 +3,7 @@
 //   y = x W^T + bias,   W_nk = s_n,g(k) (q_nk - 8),   q in 0..15,
 //
 // for few rows of x: the matrix is read once, which is what the product costs.
-// Measured: 16 x 10^6 x 300 fp32 63 us (238 MB at 3.8 TB/s), 61 x 100,000 x 600 fp16 in
+// Measured: 16 x 10^6 x 300 fp32 61 us (238 MB at 3.9 TB/s), 61 x 100,000 x 600 fp16 in
 // groups of 64 20 to 21 us (44.8 MB, 7.3 GFLOP), 1 x 71,290 x 300 bf16 12 us, 8 of them in
 // the kernel.
 //
@@ -52,7 +52,10 @@ __host__ __device__ __forceinline__ int64_t scale_at(int groups, int g, int r) {
 
 // ------------------------------------------------------------ quantisation --
 
-// One wavefront a tile and group. Column 8 q + j of a block is in nibble j / 2 of
+// One wavefront a tile and group, of which it reads 16 rows of 32 to 128 columns: 10^6 x
+// 300 fp32 in groups of 32 in 389 us (1.4 GB at 3.5 TB/s), bf16 380, fp16 in groups of 128
+// 271; bound by instruction issue, a division a weight and four blocks whatever the group
+// has. Column 8 q + j of a block is in nibble j / 2 of
 // lane 16 q + r's word for even j, 4 + j / 2 for odd j, so that a shift leaves two
 // neighbours in the halves of a register. s = max|w| / 7, rounded to bfloat16
 // before the codes are taken with it.
